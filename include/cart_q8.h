@@ -1,0 +1,125 @@
+/*
+ * cart_q8.h -- key/value caches in 8 bits: the part of libcart.so's C ABI that stores tokens as codes with a scale,
+ * reads them back and attends over them.
+ *
+ * A cache (cart_q8) is to 8-bit storage what a Cartridge and a request's suffix are to bf16 storage (Sec. 3.2, Sec. 3.3
+ * of arXiv 2506.06266): an append-only sequence of tokens for every layer and KV head, in pages of CART_PAGE_TOKENS
+ * tokens taken from the context's arena.  It may stand behind other caches, its parts: a query of the cache attends
+ * over [part_1 ; part_2 ; ... ; the cache's own tokens].  A Cartridge in 8 bits is a cache that is written once and
+ * then named as a part by many; a request is a cache opened behind its Cartridge(s).  Half the bytes of bf16 means
+ * twice the Cartridges and users per arena, and half the time of a decode step that is bound by HBM.
+ *
+ * Format.  CART_Q8_BLOCK_TOKENS = 16 consecutive tokens of one KV head share one scale 2^e for their keys and one for
+ * their values.  A value x is stored as the code nearest to x * 2^-e, ties to even: an integer of -127 .. 127
+ * (CART_Q8_INT8) or a finite e4m3 number of magnitude up to 448 (CART_Q8_E4M3).  e is the smallest integer >= -120 for
+ * which no value of the block leaves that range.  Powers of two make scaling exact: what a code stands for, code * 2^e,
+ * is a bf16 number, so cart_q8_read returns it exactly and attention uses exactly it.  (A scale of max / 127 would use
+ * up to one bit more of int8's range; it would round twice in reading, and a block whose scale grows would drift.)
+ * The error of a value is at most 2^(e-1) in int8; in e4m3 at most 2^-4 of the value, or 2^(e-10) where that is more.
+ *   - Tokens that join a block which holds some already can only raise its e.  When they do, the codes it holds are
+ *     rounded once more, to the larger step: since every raise at least doubles the step, the error of an int8 value
+ *     stays below 2^e however often its block's scale grows.  e falls again only when the block is begun anew, with its
+ *     first token.
+ *   - A block into which a NaN or an infinity is written has no scale; all of its values read as NaN until it is begun
+ *     anew.
+ *
+ * Conventions are those of cart.h: host-side checks before anything is launched, statuses, errors by cart_last_error,
+ * streams, one driving thread and stream at a time, device memory from the arena only.  Tensors are bf16, head_dim =
+ * 128.  The calls run on the context's device whichever device is current.  They keep lengths on the host and upload page lists as these change, so they cannot be
+ * captured into a CUDA graph: on a stream that is being captured they return CART_ERR_INVALID_ARG.
+ */
+#ifndef CART_Q8_H_
+#define CART_Q8_H_
+
+#include "cart.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef int32_t cart_q8; /* handle of a cache in 8 bits */
+
+#define CART_Q8_INT8 0
+#define CART_Q8_E4M3 1
+#define CART_Q8_BLOCK_TOKENS 16
+
+/* Bytes of the arena that the 8-bit calls take for their own tables (page lists, work lists, split partials) when the
+ * first cache is opened; they stay taken until cart_destroy.  Pure host arithmetic.  Errors: INVALID_ARG, SHAPE. */
+CART_API cart_status cart_q8_scratch_bytes(const cart_config *cfg /*host*/, uint64_t *out_bytes /*host*/);
+
+/* Bytes of the arena that a cache of n_tokens tokens in every layer takes (whole pages; n_tokens >= 0).  Pure host
+ * arithmetic.  Errors: INVALID_ARG, SHAPE. */
+CART_API cart_status cart_q8_cache_bytes(const cart_config *cfg /*host*/, int32_t n_tokens, uint64_t *out_bytes /*host*/);
+
+/* Opens an empty cache behind n_parts others (host array, in order, may be NULL when 0; a part that has parts of its own
+ * stands for [its parts ; its tokens]).  All have the same format.  While another cache stands behind it a part may not
+ * be written or closed (CART_ERR_IN_USE).  Pages for `capacity` tokens (>= 0) are taken now, further ones as tokens are
+ * written.  Errors: INVALID_ARG (format, capacity), BAD_HANDLE, CAPACITY (more than max_parts parts, flattened), OOM,
+ * CUDA. */
+CART_API cart_status cart_q8_open(cart_ctx *ctx, int32_t format, const cart_q8 *parts /*host*/, int32_t n_parts,
+                                  int32_t capacity, cart_q8 *out /*host*/);
+
+/* Gives a cache's pages back to the arena; the caller makes sure that no enqueued call still reads them (later calls on
+ * the same stream may).  Errors: BAD_HANDLE, IN_USE (it is a part of another cache). */
+CART_API cart_status cart_q8_close(cart_ctx *ctx, cart_q8 id);
+
+/* Quantises a registered Cartridge: a cache that holds its p tokens in every layer, as cart_q8_write would store them.
+ * The Cartridge stays as it is (it may be released afterwards).  Errors: BAD_HANDLE (also: a composition), EVICTED,
+ * INVALID_ARG, OOM, CUDA. */
+CART_API cart_status cart_q8_from_cartridge(cart_ctx *ctx, cart_id cartridge, int32_t format, void *stream,
+                                            cart_q8 *out /*host*/);
+
+/* Quantises tokens into caches, in one layer (Sec. 2.3: a decode step's token, or the tokens of a message).  ids, first,
+ * n_tokens are host arrays of n_ids entries; a handle may appear at most once.  Cache i receives n_tokens[i] >= 0 tokens
+ * at the positions first[i] .. first[i] + n_tokens[i] - 1, where 0 <= first[i] <= its length in `layer`; its length
+ * becomes first[i] + n_tokens[i], so tokens behind that are dropped (a rejected draft is written over).  first = NULL
+ * appends.  k and v hold the tokens of all caches back to back on one token axis: the 128 values of token t, KV head h
+ * are at element t * token_stride + h * head_stride (strides in bf16 elements, >= 0, multiples of 8: slices of a fused
+ * projection will do).  With no token at all nothing is launched and k and v may be NULL.
+ * Errors: INVALID_ARG, BAD_HANDLE (handle, layer), IN_USE (the cache is a part of another), OOM (no page left; nothing
+ * has changed), CAPACITY (the batch names more pages than a call can list), CUDA. */
+CART_API cart_status cart_q8_write(cart_ctx *ctx, int32_t layer, const cart_q8 *ids /*host*/, int32_t n_ids,
+                                   const int32_t *first /*host or NULL*/, const int32_t *n_tokens /*host*/,
+                                   const void *k /*device*/, const void *v /*device*/, int64_t token_stride,
+                                   int64_t head_stride, void *stream);
+
+/* Reads caches back: what their codes stand for, as bf16 (exact).  Cache i gives its own tokens first[i] .. first[i] +
+ * n_tokens[i] - 1 in `layer` (n_tokens[i] >= 0; a handle may appear more than once); k and v receive them back to back,
+ * [sum of n_tokens][n_kv_heads][128].  Errors: INVALID_ARG (also: a range beyond the cache's length), BAD_HANDLE,
+ * CAPACITY, CUDA. */
+CART_API cart_status cart_q8_read(cart_ctx *ctx, int32_t layer, const cart_q8 *ids /*host*/, int32_t n_ids,
+                                  const int32_t *first /*host*/, const int32_t *n_tokens /*host*/, void *k /*device*/,
+                                  void *v /*device*/, void *stream);
+
+/* Eq. 1 (Sec. 2.3) over caches in 8 bits, for a batch of decoding requests, messages, or both: the queries are the last
+ * n_new[i] tokens of cache i (n_new = NULL: one each).  Row r of a cache's n_new rows sees its parts and its own tokens
+ * except the last n_new[i] - 1 - r (the causal sum over j <= i); write the tokens first.  n_new[i] = 0 leaves a cache
+ * out; n_new[i] may exceed its own length only by being 1 (a query over the parts alone).  q and out are device bf16
+ * [sum of n_new][n_q_heads][128], lse device fp32 [sum of n_new][n_q_heads] (natural log) or NULL: rows back to back,
+ * cache after cache; nothing behind the last row is touched.  ids, n_new are host arrays; duplicate handles are allowed.
+ * Parts that many rows of the batch have in common are read once for up to 128 / G of them (as cart_set_share_min_readers
+ * says for cart_decode_attention).  Sums, maxima and the output are kept in fp32; results are bitwise reproducible for
+ * the same sequence of calls.  A query row that holds a NaN or an infinity gives NaN.
+ * Errors: INVALID_ARG, BAD_HANDLE, EMPTY (a row would see no token), CAPACITY (more rows than max_requests, or more
+ * pages than a call can list), CUDA. */
+CART_API cart_status cart_q8_attention(cart_ctx *ctx, int32_t layer, const cart_q8 *ids /*host*/, int32_t n_ids,
+                                       const int32_t *n_new /*host or NULL*/, const void *q /*device*/,
+                                       void *out /*device*/, float *lse /*device or NULL*/, void *stream);
+
+/* One decode step of a layer (Sec. 2.3): cart_q8_write of one token per cache (k_new, v_new device bf16
+ * [n_ids][n_kv_heads][128], at first[i] or appended), then cart_q8_attention with one query each.
+ * Errors: those of the two; on an error nothing is written. */
+CART_API cart_status cart_q8_decode_step(cart_ctx *ctx, int32_t layer, const cart_q8 *ids /*host*/, int32_t n_ids,
+                                         const int32_t *first /*host or NULL*/, const void *k_new /*device*/,
+                                         const void *v_new /*device*/, const void *q /*device*/, void *out /*device*/,
+                                         float *lse /*device or NULL*/, void *stream);
+
+/* A cache's own length in a layer, and what a query of it sees (its parts included); either pointer may be NULL.
+ * Errors: BAD_HANDLE. */
+CART_API cart_status cart_q8_len(cart_ctx *ctx, cart_q8 id, int32_t layer, int32_t *own /*host or NULL*/,
+                                 int64_t *total /*host or NULL*/);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* CART_Q8_H_ */

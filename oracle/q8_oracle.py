@@ -1,0 +1,129 @@
+"""Float64 definitions of the caches in 8 bits (test infrastructure only): what a cache stands for after a series of
+writes, attention over caches, and how far a result in bf16 / fp32 may be from it.  Written from the format's definition
+(include/cart_q8.h) with explicit loops over blocks and rows; shares no code with the library."""
+from __future__ import annotations
+
+import math
+from typing import List, Sequence, Tuple
+
+import numpy as np
+
+BLOCK = 16
+E_MIN = -120
+TOP = {"int8": 127.0, "e4m3": 448.0}
+
+
+def to_grid(y: np.ndarray, fmt: str) -> np.ndarray:
+    """The nearest value that a code has (ties to the even code); y is already divided by the scale."""
+    if fmt == "int8":
+        return np.rint(y)
+    mag = np.maximum(np.abs(y), 2.0 ** -6)               # below 2^-6 the steps stay those of [2^-6, 2^-5)
+    step = 2.0 ** (np.floor(np.log2(mag)) - 3)
+    return np.rint(y / step) * step
+
+
+def exponent(block: np.ndarray, fmt: str) -> int:
+    """The smallest e >= E_MIN with max |x| <= TOP 2^e."""
+    big = float(np.max(np.abs(block))) if block.size else 0.0
+    e = E_MIN
+    if big > 0:
+        e = max(E_MIN, math.frexp(big)[1] - 10)           # a lower bound, then counted up
+        while big > TOP[fmt] * 2.0 ** e:
+            e += 1
+    return e
+
+
+class Cache:
+    """One layer of one cache: codes (as numbers) and exponents of keys and values, [block][head]."""
+
+    def __init__(self, fmt: str, n_heads: int, parts: Sequence["Cache"] = ()):
+        self.fmt, self.H = fmt, n_heads
+        self.parts: List[Cache] = [q for p in parts for q in (*p.parts, p)]
+        self.n = 0
+        self.codes = [np.zeros((0, n_heads, 128)) for _ in range(2)]
+        self.exps: List[List[List]] = [[], []]            # [keys / values][block][head]: exponent or None (no scale)
+
+    def write(self, k: np.ndarray, v: np.ndarray, first=None) -> None:
+        first = self.n if first is None else first
+        m = k.shape[0]
+        for x in range(2):
+            new = (k, v)[x].astype(np.float64)
+            codes = np.concatenate([self.codes[x][:first], np.zeros((m, self.H, 128))])
+            exps = self.exps[x][: (first + BLOCK - 1) // BLOCK]
+            for b in range(first // BLOCK, (first + m + BLOCK - 1) // BLOCK if m else 0):
+                lo, hi = b * BLOCK, min((b + 1) * BLOCK, first + m)
+                mid = max(lo, first)                       # tokens lo .. mid are held, mid .. hi are new
+                if b == len(exps):
+                    exps = exps + [[E_MIN] * self.H]
+                row = list(exps[b])
+                for h in range(self.H):
+                    y = new[mid - first:hi - first, h]
+                    old = row[h]
+                    if old is None or not np.all(np.isfinite(y)):
+                        row[h] = None
+                        continue
+                    e = max(exponent(y, self.fmt), old if mid > lo else E_MIN)
+                    codes[lo:mid, h] = to_grid(codes[lo:mid, h] * 2.0 ** (old - e), self.fmt)
+                    codes[mid:hi, h] = to_grid(y * 2.0 ** -e, self.fmt)
+                    row[h] = e
+                if mid == lo:                              # begun anew: an earlier mark does not count
+                    for h in range(self.H):
+                        y = new[mid - first:hi - first, h]
+                        if np.all(np.isfinite(y)):
+                            e = exponent(y, self.fmt)
+                            codes[mid:hi, h] = to_grid(y * 2.0 ** -e, self.fmt)
+                            row[h] = e
+                        else:
+                            row[h] = None
+                exps = exps[:b] + [row] + exps[b + 1:]
+            self.codes[x], self.exps[x] = codes, exps
+        self.n = first + m
+
+    def values(self, x: int) -> np.ndarray:
+        """[n][heads][128]; NaN where a block has no scale."""
+        s = np.array([[np.nan if e is None else 2.0 ** e for e in row] for row in self.exps[x]]).reshape(-1, self.H)
+        return self.codes[x] * np.repeat(s, BLOCK, axis=0)[: self.n, :, None]
+
+    def seen(self, x: int) -> np.ndarray:
+        return np.concatenate([p.values(x) for p in self.parts] + [self.values(x)])
+
+    def scales(self, x: int) -> np.ndarray:
+        """[tokens seen][heads]"""
+        return np.concatenate([np.repeat(np.array([[np.nan if e is None else 2.0 ** e for e in r] for r in c.exps[x]]).reshape(-1, self.H),
+                                         BLOCK, axis=0)[: c.n] for c in (*self.parts, self)])
+
+
+def attention(cache: Cache, q: np.ndarray, scale: float) -> Tuple[np.ndarray, ...]:
+    """q [n_new][Hq][128] -> out, lse, and the errors that a kernel's roundings may cause in each.
+
+    The kernel's products are exact in each term (codes and the scaled query are fp16 numbers) and summed in fp32; so a score is
+    off by at most d = 130 * 2^-24 * scale sum|q k| + 8 * 2^-24 |s| (sum, scaling, base change, subtraction of the reference),
+    and a query's elements below 2^-14 of its largest add 2^-25 of that largest per key value.  A probability is then off by
+    d + 2^-21 relatively (exponential).  It is rounded to fp16 relative to the largest (probability times scale of its
+    values): 2^-11 relatively, and below 2^-14 of the largest at most 2^-25 of it.  (A kernel that rounds probabilities to
+    bf16: 2^-8 relatively, no smallest one.)  The output is rounded to bf16, 2^-8 relatively."""
+    k, v, s2 = cache.seen(0), cache.seen(1), cache.scales(1)
+    n_new, Hq = q.shape[:2]
+    G = Hq // cache.H
+    n = k.shape[0]
+    out, lse = np.empty((n_new, Hq, 128)), np.empty((n_new, Hq))
+    tol, tol_lse = np.empty_like(out), np.empty_like(lse)
+    for r in range(n_new):
+        end = n - (n_new - 1 - r)
+        for h in range(Hq):
+            kk, vv, sv = k[:end, h // G], v[:end, h // G], s2[:end, h // G]
+            x = q[r, h].astype(np.float64)
+            s = scale * (kk @ x)
+            m = np.max(s)
+            p = np.exp(s - m)
+            L = np.sum(p)
+            out[r, h] = (p @ vv) / L
+            lse[r, h] = m + np.log(L)
+            d = 130 * 2.0 ** -24 * scale * (np.abs(kk) @ np.abs(x)) + 8 * 2.0 ** -24 * np.abs(s)
+            d = d + scale * 2.0 ** -25 * np.max(np.abs(x)) * np.sum(np.abs(kk), axis=1)
+            d = np.max(d * (p > 1e-30)) + 2.0 ** -21
+            tol_lse[r, h] = d + 2.0 ** -21 + 8 * 2.0 ** -24 * abs(lse[r, h])
+            spread = (p @ np.abs(vv)) / L
+            small = end * 2.0 ** -25 * TOP[cache.fmt] * np.max(p * sv) / L
+            tol[r, h] = 2.0 ** -8 * np.abs(out[r, h]) + (2.0 ** -8 + 3 * d) * spread * 1.01 + small + 2.0 ** -130
+    return out, lse, tol, tol_lse

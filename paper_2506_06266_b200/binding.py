@@ -24,6 +24,8 @@ STATUS_NAMES = ["CART_OK", "CART_ERR_INVALID_ARG", "CART_ERR_SHAPE", "CART_ERR_B
 (CART_ERR_INVALID_ARG, CART_ERR_SHAPE, CART_ERR_BAD_HANDLE, CART_ERR_CAPACITY, CART_ERR_OOM,
  CART_ERR_EMPTY, CART_ERR_IN_USE, CART_ERR_CUDA, CART_ERR_TIMEOUT, CART_ERR_EVICTED) = range(1, 11)
 CART_PAGE_TOKENS = 64
+CART_Q8_INT8, CART_Q8_E4M3 = 0, 1
+CART_Q8_BLOCK_TOKENS = 16
 
 # every symbol include/cart.h and include/cart_plan.h declare
 EXPORTS = ["cart_scratch_bytes", "cart_create", "cart_destroy", "cart_register_cartridge",
@@ -35,7 +37,9 @@ EXPORTS = ["cart_scratch_bytes", "cart_create", "cart_destroy", "cart_register_c
            "cart_request_open_paged", "cart_evict_request", "cart_restore_request", "cart_evict_cartridge",
            "cart_restore_cartridge", "cart_train_attention_fwd", "cart_train_attention_bwd",
            "cart_decode_attention_static", "cart_launch_count", "cart_status_string",
-           "cart_last_error", "cart_plan_build"]
+           "cart_last_error", "cart_plan_build",
+           "cart_q8_scratch_bytes", "cart_q8_cache_bytes", "cart_q8_open", "cart_q8_close", "cart_q8_from_cartridge",
+           "cart_q8_write", "cart_q8_read", "cart_q8_attention", "cart_q8_decode_step", "cart_q8_len"]
 
 
 class cart_config(ctypes.Structure):
@@ -164,6 +168,17 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.cart_status_string.restype = ctypes.c_char_p
     lib.cart_last_error.argtypes = [vp]
     lib.cart_last_error.restype = ctypes.c_char_p
+    i64, i64p = ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)
+    lib.cart_q8_scratch_bytes.argtypes = [ctypes.POINTER(cart_config), u64p]
+    lib.cart_q8_cache_bytes.argtypes = [ctypes.POINTER(cart_config), i32, u64p]
+    lib.cart_q8_open.argtypes = [vp, i32, i32p, i32, i32, i32p]
+    lib.cart_q8_close.argtypes = [vp, i32]
+    lib.cart_q8_from_cartridge.argtypes = [vp, i32, i32, vp, i32p]
+    lib.cart_q8_write.argtypes = [vp, i32, i32p, i32, i32p, i32p, vp, vp, i64, i64, vp]
+    lib.cart_q8_read.argtypes = [vp, i32, i32p, i32, i32p, i32p, vp, vp, vp]
+    lib.cart_q8_attention.argtypes = [vp, i32, i32p, i32, i32p, vp, vp, vp, vp]
+    lib.cart_q8_decode_step.argtypes = [vp, i32, i32p, i32, i32p, vp, vp, vp, vp, vp, vp]
+    lib.cart_q8_len.argtypes = [vp, i32, i32, i32p, i64p]
     lib.cart_plan_build.argtypes = [
         ctypes.POINTER(cart_plan_seg), i32p, i32, i32, i32, i32, ctypes.POINTER(cart_work_item), i32,
         i32p, ctypes.POINTER(ctypes.c_uint32), ctypes.POINTER(cart_merge_item), i32, i32p, i32p, i32p,
@@ -430,6 +445,108 @@ def cart_decode_attention_static(q, kv, n_reqs: int, n_q_heads: int, n_kv_heads:
     _check(load_library().cart_decode_attention_static(
         _ptr(q), _ptr(kv), int(n_reqs), int(n_q_heads), int(n_kv_heads), int(n_tokens), float(softmax_scale),
         _ptr(out), _ptr(lse), int(device), _stream(stream)), "cart_decode_attention_static")
+
+
+# ---- caches in 8 bits (include/cart_q8.h) ----------------------------------------------------------------------------
+
+def _q8_tensor(x, name: str) -> None:
+    """A torch tensor handed to the 8-bit calls must be what the C side takes it for: bf16, dense (addresses are trusted)."""
+    if not hasattr(x, "data_ptr"):
+        return
+    if str(x.dtype) != "torch.bfloat16":
+        raise ValueError("%s must be bfloat16, not %s" % (name, x.dtype))
+    if not x.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+
+
+def _counts(xs, n: int, name: str):
+    """A host array of one integer per cache (a ReqList, marshalled once, or a sequence); None stays None."""
+    if xs is None:
+        return None
+    arr, m = _reqs(xs)
+    if m != n:
+        raise ValueError("%s has %d entries for %d caches" % (name, m, n))
+    return arr
+
+
+def cart_q8_scratch_bytes(cfg: cart_config) -> int:
+    out = ctypes.c_uint64(0)
+    _check(load_library().cart_q8_scratch_bytes(ctypes.byref(cfg), ctypes.byref(out)), "cart_q8_scratch_bytes")
+    return int(out.value)
+
+
+def cart_q8_cache_bytes(cfg: cart_config, n_tokens: int) -> int:
+    out = ctypes.c_uint64(0)
+    _check(load_library().cart_q8_cache_bytes(ctypes.byref(cfg), int(n_tokens), ctypes.byref(out)), "cart_q8_cache_bytes")
+    return int(out.value)
+
+
+def cart_q8_open(ctx: int, fmt: int, parts: Sequence[int] = (), capacity: int = 0) -> int:
+    arr, n = _ids(parts)
+    out = ctypes.c_int32(-1)
+    _check(load_library().cart_q8_open(ctx, int(fmt), arr, n, int(capacity), ctypes.byref(out)), "cart_q8_open", ctx)
+    return int(out.value)
+
+
+def cart_q8_close(ctx: int, cid: int) -> None:
+    _check(load_library().cart_q8_close(ctx, int(cid)), "cart_q8_close", ctx)
+
+
+def cart_q8_from_cartridge(ctx: int, cartridge: int, fmt: int, stream=None) -> int:
+    out = ctypes.c_int32(-1)
+    _check(load_library().cart_q8_from_cartridge(ctx, int(cartridge), int(fmt), _stream(stream), ctypes.byref(out)),
+           "cart_q8_from_cartridge", ctx)
+    return int(out.value)
+
+
+def cart_q8_write(ctx: int, layer: int, ids, n_tokens, k, v, first=None, strides: Optional[Tuple[int, int]] = None,
+                  stream=None) -> None:
+    """k, v: bf16 [tokens][KV heads][128], torch tensors of any (equal) token and head strides, or addresses with
+    strides=(token, head) in elements."""
+    arr, n = _reqs(ids)
+    if strides is None:
+        if k is None:
+            strides = (0, 0)
+        else:
+            if str(k.dtype) != "torch.bfloat16" or k.dtype != v.dtype:
+                raise ValueError("k and v must be bfloat16, not %s and %s" % (k.dtype, v.dtype))
+            if k.dim() != 3 or k.stride() != v.stride() or k.shape != v.shape or k.shape[2] != 128 or k.stride(2) != 1:
+                raise ValueError("k and v must be [tokens][KV heads][128] of equal strides, dense in the last dimension")
+            strides = (k.stride(0), k.stride(1))
+    _check(load_library().cart_q8_write(ctx, int(layer), arr, n, _counts(first, n, "first"), _counts(n_tokens, n, "n_tokens"),
+                                        _ptr(k), _ptr(v), int(strides[0]), int(strides[1]), _stream(stream)),
+           "cart_q8_write", ctx)
+
+
+def cart_q8_read(ctx: int, layer: int, ids, first, n_tokens, k, v, stream=None) -> None:
+    arr, n = _reqs(ids)
+    _q8_tensor(k, "k")
+    _q8_tensor(v, "v")
+    _check(load_library().cart_q8_read(ctx, int(layer), arr, n, _counts(first, n, "first"), _counts(n_tokens, n, "n_tokens"),
+                                       _ptr(k), _ptr(v), _stream(stream)), "cart_q8_read", ctx)
+
+
+def cart_q8_attention(ctx: int, layer: int, ids, q, out, lse=None, n_new=None, stream=None) -> None:
+    arr, n = _reqs(ids)
+    _q8_tensor(q, "q")
+    _q8_tensor(out, "out")
+    _check(load_library().cart_q8_attention(ctx, int(layer), arr, n, _counts(n_new, n, "n_new"), _ptr(q), _ptr(out), _ptr(lse),
+                                            _stream(stream)), "cart_q8_attention", ctx)
+
+
+def cart_q8_decode_step(ctx: int, layer: int, ids, k_new, v_new, q, out, lse=None, first=None, stream=None) -> None:
+    arr, n = _reqs(ids)
+    for x, name in ((k_new, "k_new"), (v_new, "v_new"), (q, "q"), (out, "out")):
+        _q8_tensor(x, name)
+    _check(load_library().cart_q8_decode_step(ctx, int(layer), arr, n, _counts(first, n, "first"), _ptr(k_new), _ptr(v_new),
+                                              _ptr(q), _ptr(out), _ptr(lse), _stream(stream)), "cart_q8_decode_step", ctx)
+
+
+def cart_q8_len(ctx: int, cid: int, layer: int) -> Tuple[int, int]:
+    """(the cache's own tokens, the tokens that a query of it sees)"""
+    a, b = ctypes.c_int32(0), ctypes.c_int64(0)
+    _check(load_library().cart_q8_len(ctx, int(cid), int(layer), ctypes.byref(a), ctypes.byref(b)), "cart_q8_len", ctx)
+    return int(a.value), int(b.value)
 
 
 def cart_launch_count(ctx: int) -> int:

@@ -188,6 +188,7 @@ struct cart_ctx {
     bool timing = false;
     std::vector<cudaEvent_t> ev_pool;  // pairs: start, stop
     size_t ev_used = 0;
+    Q8State *q8 = nullptr;       // caches in 8 bits (cart_q8.cc), made when the first one is opened
     char err[256] = {0};
 };
 
@@ -456,6 +457,7 @@ cart_status cart_destroy(cart_ctx *ctx)
         if (sl.ev) cudaEventDestroy(sl.ev);
     }
     for (cudaEvent_t e : ctx->ev_pool) cudaEventDestroy(e);
+    q8_release(ctx->q8);
     delete ctx;
     return CART_OK;
 }
@@ -2047,9 +2049,56 @@ cart_status cart_sync_status(cart_ctx *ctx, void *stream)
     if (word != 0) {
         // a block that gave up may have left arrival tickets behind: clear them with the word
         CART_CUDA(ctx, cudaMemset(st, 0, ctx->lay.plan_off));
+        q8_clear_tickets(ctx);
         return fail(ctx, CART_ERR_TIMEOUT, "a device-side wait ran out (status word 0x%x)", word);
     }
     return CART_OK;
 }
 
 }  // extern "C"
+
+namespace cart {
+
+CtxView ctx_view(cart_ctx *ctx)
+{
+    CtxView v{};
+    v.cfg = &ctx->cfg;
+    v.group = ctx->group;
+    v.scale = ctx->scale;
+    v.n_cta = ctx->n_cta;
+    v.share_min_readers = ctx->share_min_readers;
+    v.piece_cost = ctx->piece_cost;
+    v.unit_cost = kUnitCostTiles;
+    v.side_by_side = ctx->side_by_side;
+    v.max_grow = ctx->max_grow;
+    v.launches = &ctx->launches;
+    v.status = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(ctx->cfg.arena) + ctx->lay.status_off);
+    v.n_rows = ctx->n_rows;
+    v.q8 = &ctx->q8;
+    return v;
+}
+
+cart_status ctx_fail(cart_ctx *ctx, cart_status st, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(ctx->err, sizeof ctx->err, fmt, ap);
+    va_end(ap);
+    return st;
+}
+
+bool ctx_arena_alloc(cart_ctx *ctx, uint64_t rows, uint64_t *start) { return arena_alloc(ctx, rows, start); }
+void ctx_arena_free(cart_ctx *ctx, uint64_t start, uint64_t rows) { arena_free(ctx, start, rows); }
+
+cart_status ctx_cartridge(cart_ctx *ctx, cart_id id, uint64_t *k_row, uint64_t *v_row, int32_t *p)
+{
+    const Cartridge *c = get_cart(ctx, id);
+    if (!c || c->composed) return CART_ERR_BAD_HANDLE;
+    if (c->evicted) return CART_ERR_EVICTED;
+    *k_row = c->k_row;
+    *v_row = c->v_row;
+    *p = c->p;
+    return CART_OK;
+}
+
+}  // namespace cart

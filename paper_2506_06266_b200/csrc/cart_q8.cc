@@ -1,0 +1,830 @@
+// Host side of the caches in 8 bits: handles, pages, plans and launches.  The contract is in include/cart_q8.h.
+#include <algorithm>
+#include <climits>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "cart_q8_internal.h"
+
+namespace cart {
+
+namespace {
+
+constexpr int kQ8MaxCta = 1024;
+constexpr int kQ8Slots = 4;      // uploaded plans and page lists
+constexpr uint64_t kQ8Align = 256;
+
+uint64_t up(uint64_t x) { return (x + kQ8Align - 1) / kQ8Align * kQ8Align; }
+
+// One slot: [cta_begin][merges][items] [unit_cta_begin][readers][reader_slot][reader_merge][units] [pages]; then, behind
+// the slots, the split partials, and in front of them the arrival tickets.  A function of the configuration alone.
+struct Q8Layout {
+    uint64_t tickets_bytes;
+    uint64_t merges_off, items_off, unit_cta_off, readers_off, reader_slot_off, reader_merge_off, units_off, pages_off;
+    uint64_t slot_bytes, part_o_off, part_lse_off, total;
+    int items_cap, merges_cap, slots_cap, units_cap, readers_cap, pages_cap;
+};
+
+Q8Layout q8_layout(const cart_config &c)
+{
+    Q8Layout s{};
+    const int parts = c.max_parts > 0 ? c.max_parts : 8;
+    const int group = c.n_q_heads / c.n_kv_heads;
+    const int row_groups = c.max_requests * c.n_kv_heads;
+    // as for the bf16 plans: a row group owns at most parts + 2 segments, a block boundary cuts an item in two
+    s.items_cap = row_groups * (parts + 2) + kQ8MaxCta;
+    s.merges_cap = row_groups + kQ8MaxCta;
+    s.slots_cap = 10 * row_groups + 2 * kQ8MaxCta;
+    s.readers_cap = c.max_requests * (parts + 1);
+    s.units_cap = s.readers_cap * c.n_kv_heads + kQ8MaxCta;
+    s.pages_cap = 256 * c.max_requests + 65536;  // 16 k tokens a request on average, and 4 M tokens besides
+    s.tickets_bytes = up((uint64_t)s.merges_cap * 4);
+    s.merges_off = up((uint64_t)(kQ8MaxCta + 1) * 4);
+    s.items_off = s.merges_off + up((uint64_t)s.merges_cap * sizeof(cart_merge_item));
+    s.unit_cta_off = s.items_off + up((uint64_t)s.items_cap * sizeof(cart_work_item));
+    s.readers_off = s.unit_cta_off + up((uint64_t)(kQ8MaxCta + 1) * 4);
+    s.reader_slot_off = s.readers_off + up((uint64_t)s.readers_cap * 4);
+    s.reader_merge_off = s.reader_slot_off + up((uint64_t)s.readers_cap * c.n_kv_heads * 4);
+    s.units_off = s.reader_merge_off + up((uint64_t)s.readers_cap * c.n_kv_heads * 4);
+    s.pages_off = s.units_off + up((uint64_t)s.units_cap * sizeof(cart_shared_unit));
+    s.slot_bytes = s.pages_off + up((uint64_t)s.pages_cap * 4);
+    s.part_o_off = s.tickets_bytes + (uint64_t)kQ8Slots * s.slot_bytes;
+    s.part_lse_off = s.part_o_off + up((uint64_t)s.slots_cap * group * kHeadDim * 4);
+    s.total = s.part_lse_off + up((uint64_t)s.slots_cap * kMaxGroup * 4);
+    return s;
+}
+
+uint64_t page_bytes(const cart_config &c) { return up((uint64_t)c.n_layers * c.n_kv_heads * kQ8HeadBytes); }
+
+cart_status check(const cart_config *c)
+{
+    uint64_t unused;
+    return cart_scratch_bytes(c, &unused);  // the same rules
+}
+
+struct Cache {
+    bool live = false;
+    int32_t format = 0;
+    std::vector<int32_t> parts;    // flattened, in order
+    std::vector<int32_t> len;      // per layer
+    std::vector<uint32_t> pages;   // base rows
+    int32_t refs = 0;              // caches that stand behind this one
+    uint64_t stamp = 0;
+    uint64_t list_stamp = 0;       // building a page list: the cache's pages are in it, from list_base on
+    uint32_t list_base = 0;
+    int64_t cap() const { return (int64_t)pages.size() * kTileTokens; }
+};
+
+enum SlotKind { kNothing, kList, kDecode, kMessage };
+
+struct Slot {
+    uint8_t *host = nullptr;  // pinned
+    uint8_t *dev = nullptr;   // arena
+    cudaEvent_t ev = nullptr;
+    bool ev_recorded = false, used_since = false;
+    SlotKind kind = kNothing;
+    uint64_t epoch = 0, used = 0;
+    cudaStream_t last_stream = nullptr;
+    std::vector<int32_t> key;     // what it was built for, besides lens
+    std::vector<int32_t> lens;    // kDecode: own lengths when it was built
+    std::vector<uint32_t> bases;  // per cache of the call: index of its page 0 in the page list
+    int32_t n_items = 0, n_merges = 0, n_cta_used = 0, n_units = 0, n_unit_cta_used = 0;
+};
+
+}  // namespace
+
+struct Q8State {
+    Q8Layout lay{};
+    uint64_t start = 0, rows = 0;  // the arena rows that it took
+    uint8_t *base = nullptr;
+    std::vector<Cache> caches;
+    Slot slots[kQ8Slots];
+    uint64_t epoch = 1, stamp = 0, list_stamp = 0, clock = 0;
+    std::vector<int32_t> key_tmp, len_tmp, seg_begin_tmp, first_tmp, cnt_tmp;
+    std::vector<cart_plan_seg> seg_tmp;
+};
+
+void q8_release(Q8State *st)
+{
+    if (!st) return;
+    for (Slot &s : st->slots) {
+        if (s.host) cudaFreeHost(s.host);
+        if (s.ev) cudaEventDestroy(s.ev);
+    }
+    delete st;
+}
+
+void q8_clear_tickets(cart_ctx *ctx)
+{
+    Q8State *st = *ctx_view(ctx).q8;
+    if (st) (void)cudaMemset(st->base, 0, st->lay.tickets_bytes);
+}
+
+namespace {
+
+#define Q8_CUDA(ctx, call)                                                                          \
+    do {                                                                                            \
+        cudaError_t e_ = (call);                                                                    \
+        if (e_ != cudaSuccess)                                                                      \
+            return ctx_fail(ctx, CART_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));    \
+    } while (0)
+
+// The context's device while a call runs.
+struct OnDevice {
+    int before = -1;
+    bool changed = false;
+    explicit OnDevice(int device)
+    {
+        if (cudaGetDevice(&before) == cudaSuccess && before != device) changed = cudaSetDevice(device) == cudaSuccess;
+    }
+    ~OnDevice()
+    {
+        if (changed) cudaSetDevice(before);
+    }
+};
+
+bool aligned16(const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+cart_status not_capturing(cart_ctx *ctx, cudaStream_t s, const char *what)
+{
+    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+    const cudaError_t e = cudaStreamIsCapturing(s, &cs);
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return ctx_fail(ctx, e == cudaErrorStreamCaptureImplicit ? CART_ERR_INVALID_ARG : CART_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+    }
+    if (cs != cudaStreamCaptureStatusNone) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "%s: the stream is being captured", what);
+    return CART_OK;
+}
+
+cart_status make_state(cart_ctx *ctx)
+{
+    const CtxView v = ctx_view(ctx);
+    if (*v.q8) return CART_OK;
+    Q8State *st = new (std::nothrow) Q8State();
+    if (!st) return ctx_fail(ctx, CART_ERR_OOM, "q8: out of host memory");
+    st->lay = q8_layout(*v.cfg);
+    st->rows = (st->lay.total + kRowBytes - 1) / kRowBytes;
+    if (!ctx_arena_alloc(ctx, st->rows, &st->start)) {
+        delete st;
+        return ctx_fail(ctx, CART_ERR_OOM, "q8: the arena has no room for the tables of the 8-bit calls");
+    }
+    st->base = static_cast<uint8_t *>(v.cfg->arena) + st->start * kRowBytes;
+    cudaError_t e = q8_prepare_kernels();
+    if (e == cudaSuccess) e = cudaMemset(st->base, 0, st->lay.tickets_bytes);
+    for (int i = 0; i < kQ8Slots && e == cudaSuccess; ++i) {
+        Slot &s = st->slots[i];
+        s.dev = st->base + st->lay.tickets_bytes + (uint64_t)i * st->lay.slot_bytes;
+        e = cudaHostAlloc(reinterpret_cast<void **>(&s.host), st->lay.slot_bytes, cudaHostAllocDefault);
+        if (e == cudaSuccess) e = cudaEventCreateWithFlags(&s.ev, cudaEventDisableTiming);
+    }
+    if (e != cudaSuccess) {
+        ctx_arena_free(ctx, st->start, st->rows);
+        q8_release(st);
+        return ctx_fail(ctx, CART_ERR_CUDA, "q8: set-up failed: %s", cudaGetErrorString(e));
+    }
+    *v.q8 = st;
+    return CART_OK;
+}
+
+Cache *get(cart_ctx *ctx, cart_q8 id)
+{
+    Q8State *st = *ctx_view(ctx).q8;
+    if (!st || id < 0 || (size_t)id >= st->caches.size() || !st->caches[(size_t)id].live) return nullptr;
+    return &st->caches[(size_t)id];
+}
+
+void drop_pages(cart_ctx *ctx, Q8State *st, Cache &c, size_t keep)
+{
+    const uint64_t rows = page_bytes(*ctx_view(ctx).cfg) / kRowBytes;
+    if (c.pages.size() > keep) ++st->epoch;
+    while (c.pages.size() > keep) {
+        ctx_arena_free(ctx, c.pages.back(), rows);
+        c.pages.pop_back();
+    }
+}
+
+// Takes pages until the cache has room for `tokens`.  False: the arena is full (what was taken stays with the cache).
+bool take_pages(cart_ctx *ctx, Q8State *st, Cache &c, int64_t tokens)
+{
+    const uint64_t rows = page_bytes(*ctx_view(ctx).cfg) / kRowBytes;
+    while (c.cap() < tokens) {
+        uint64_t start = 0;
+        if (!ctx_arena_alloc(ctx, rows, &start)) return false;
+        c.pages.push_back((uint32_t)start);
+        ++st->epoch;
+    }
+    return true;
+}
+
+// The slot whose contents go: not used for longest.  Waits until the kernels that read it are done.
+cart_status free_slot(cart_ctx *ctx, Q8State *st, Slot **out)
+{
+    Slot *old = &st->slots[0];
+    for (Slot &s : st->slots)
+        if (s.used < old->used) old = &s;
+    // the others have been used up to here: what may replace them later only has to wait for that
+    for (Slot &s : st->slots)
+        if (s.used_since) {
+            Q8_CUDA(ctx, cudaEventRecord(s.ev, s.last_stream));
+            s.used_since = false;
+            s.ev_recorded = true;
+        }
+    if (old->ev_recorded) {
+        Q8_CUDA(ctx, cudaEventSynchronize(old->ev));
+        old->ev_recorded = false;
+    }
+    old->kind = kNothing;
+    *out = old;
+    return CART_OK;
+}
+
+void use_slot(Q8State *st, Slot *s, cudaStream_t stream)
+{
+    s->used = ++st->clock;
+    s->used_since = true;
+    s->last_stream = stream;
+}
+
+// Puts a cache's pages into the list that is being made.  False: the list is full.
+bool list_pages(Q8State *st, Cache &c, uint32_t *list, uint32_t *n)
+{
+    if (c.list_stamp == st->list_stamp) return true;
+    if (*n + c.pages.size() > (size_t)st->lay.pages_cap) return false;
+    c.list_stamp = st->list_stamp;
+    c.list_base = *n;
+    if (!c.pages.empty()) std::memcpy(list + *n, c.pages.data(), c.pages.size() * 4);
+    *n += (uint32_t)c.pages.size();
+    return true;
+}
+
+// A slot that holds the page lists of the named caches (their own pages).
+cart_status list_slot(cart_ctx *ctx, const cart_q8 *ids, int32_t n, cudaStream_t s, Slot **out)
+{
+    Q8State *st = *ctx_view(ctx).q8;
+    for (Slot &sl : st->slots)
+        if (sl.kind == kList && sl.epoch == st->epoch && sl.key.size() == (size_t)n &&
+            std::memcmp(sl.key.data(), ids, (size_t)n * 4) == 0) {
+            *out = &sl;
+            return CART_OK;
+        }
+    Slot *sl = nullptr;
+    cart_status r = free_slot(ctx, st, &sl);
+    if (r != CART_OK) return r;
+    ++st->list_stamp;
+    uint32_t n_listed = 0;
+    sl->bases.clear();
+    for (int32_t i = 0; i < n; ++i) {
+        Cache &c = st->caches[(size_t)ids[i]];
+        if (!list_pages(st, c, reinterpret_cast<uint32_t *>(sl->host + st->lay.pages_off), &n_listed))
+            return ctx_fail(ctx, CART_ERR_CAPACITY, "q8: the batch names more than %d pages", st->lay.pages_cap);
+        sl->bases.push_back(c.list_base);
+    }
+    if (n_listed > 0)
+        Q8_CUDA(ctx, cudaMemcpyAsync(sl->dev + st->lay.pages_off, sl->host + st->lay.pages_off, (size_t)n_listed * 4,
+                                     cudaMemcpyHostToDevice, s));
+    use_slot(st, sl, s);  // (the copy reads the host buffer)
+    sl->key.assign(ids, ids + n);
+    sl->epoch = st->epoch;
+    sl->kind = kList;
+    *out = sl;
+    return CART_OK;
+}
+
+// Launches the write (or read) kernel over `n` caches in batches that fit the kernel's parameters.
+cart_status launch_copy(cart_ctx *ctx, bool write, const Slot *sl, int32_t layer, int32_t format, int32_t n, const int32_t *first,
+                        const int32_t *cnt, const void *k, const void *v, int64_t tok_stride, int64_t head_stride, cudaStream_t s)
+{
+    const CtxView cv = ctx_view(ctx);
+    Q8State *st = *cv.q8;
+    static_assert(sizeof(Q8CopyParams) <= 4096, "the parameters must fit the kernel parameter space");
+    Q8CopyParams p;
+    p.arena = static_cast<uint8_t *>(cv.cfg->arena);
+    p.pages = reinterpret_cast<const uint32_t *>(sl->dev + st->lay.pages_off);
+    p.k = k;
+    p.v = v;
+    p.token_stride = tok_stride;
+    p.head_stride = head_stride;
+    p.n_kv_heads = cv.cfg->n_kv_heads;
+    p.layer = layer;
+    p.format = format;
+    uint32_t src = 0;
+    for (int32_t i = 0; i < n;) {
+        uint32_t tasks = 0;
+        p.n_entries = 0;
+        for (; i < n && p.n_entries < kQ8Batch; ++i) {
+            if (cnt[i] == 0) continue;
+            const uint32_t f = (uint32_t)first[i], c = (uint32_t)cnt[i];
+            p.e[p.n_entries++] = Q8Entry{sl->bases[(size_t)i], f, c, src, tasks};
+            tasks += (f + c - 1) / kQ8Block - f / kQ8Block + 1;
+            src += c;
+        }
+        if (p.n_entries == 0) break;
+        Q8_CUDA(ctx, write ? q8_launch_write(p, tasks, s) : q8_launch_read(p, tasks, s));
+        ++*cv.launches;
+    }
+    return CART_OK;
+}
+
+// What cart_q8_write and cart_q8_decode_step check of their batch; takes the pages that the tokens need.  `had`: pages
+// per cache before (filled before any is taken).
+cart_status prepare_write(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t n_ids, const int32_t *first, const int32_t *cnt,
+                          std::vector<int32_t> *at, std::vector<size_t> *had, int32_t *format, int64_t *n_tokens, const char *what)
+{
+    const CtxView cv = ctx_view(ctx);
+    if (!ids || n_ids < 1) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "%s: empty batch", what);
+    if (layer < 0 || layer >= cv.cfg->n_layers) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "%s: layer out of range", what);
+    Q8State *st = *cv.q8;
+    if (!st) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "%s: no cache is open", what);
+    const uint64_t stamp = ++st->stamp;
+    at->clear();
+    had->clear();
+    *n_tokens = 0;
+    for (int32_t i = 0; i < n_ids; ++i) {
+        Cache *c = get(ctx, ids[i]);
+        if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "%s: ids[%d] is not an open cache", what, i);
+        if (c->stamp == stamp) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "%s: ids[%d] appears twice", what, i);
+        c->stamp = stamp;
+        if (c->refs > 0) return ctx_fail(ctx, CART_ERR_IN_USE, "%s: ids[%d] is a part of another cache", what, i);
+        if (i == 0) *format = c->format;
+        if (c->format != *format) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "%s: the caches are of different formats", what);
+        const int32_t len = c->len[(size_t)layer], f = first ? first[i] : len, m = cnt ? cnt[i] : 1;
+        if (m < 0 || f < 0 || f > len)
+            return ctx_fail(ctx, CART_ERR_INVALID_ARG, "%s: cache %d holds %d tokens: cannot write %d from %d on", what, i, len, m, f);
+        if ((int64_t)f + m > INT32_MAX - kTileTokens) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "%s: cache %d would grow too long", what, i);
+        at->push_back(f);
+        *n_tokens += m;
+    }
+    if (*n_tokens > INT32_MAX) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "%s: too many tokens", what);
+    for (int32_t i = 0; i < n_ids; ++i) had->push_back(st->caches[(size_t)ids[i]].pages.size());
+    for (int32_t i = 0; i < n_ids; ++i)
+        if (!take_pages(ctx, st, st->caches[(size_t)ids[i]], (int64_t)(*at)[(size_t)i] + (cnt ? cnt[i] : 1)))
+            return ctx_fail(ctx, CART_ERR_OOM, "%s: the arena has no page left for ids[%d]", what, i);
+    return CART_OK;
+}
+
+// Finds or makes the plan of an attention call.  n_new = null: one query per cache.
+cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t n_ids, const int32_t *n_new, bool stepping,
+                      cudaStream_t s, Slot **out, int32_t *grow)
+{
+    const CtxView cv = ctx_view(ctx);
+    Q8State *st = *cv.q8;
+    const int Hkv = cv.cfg->n_kv_heads;
+    std::vector<int32_t> &key = st->key_tmp, &lens = st->len_tmp;
+    key.clear();
+    lens.clear();
+    bool decode = true;
+    for (int32_t i = 0; i < n_ids && n_new; ++i) decode = decode && n_new[i] == 1;
+    for (int32_t i = 0; i < n_ids; ++i) {
+        const Cache &c = st->caches[(size_t)ids[i]];
+        key.push_back(ids[i]);
+        for (int32_t q : c.parts) key.push_back(st->caches[(size_t)q].len[(size_t)layer]);
+        if (!decode) key.push_back(n_new[i]);
+        lens.push_back(c.len[(size_t)layer]);
+    }
+    key.push_back(cv.share_min_readers);
+    key.push_back(cv.piece_cost);
+    key.push_back(cv.side_by_side);
+    for (Slot &sl : st->slots) {
+        if (sl.kind != (decode ? kDecode : kMessage) || sl.epoch != st->epoch || sl.key != key) continue;
+        if (decode ? cart_plan_reusable(sl.lens.data(), lens.data(), n_ids, cv.max_grow, grow) != 0 : sl.lens == lens) {
+            if (!decode) *grow = 0;
+            *out = &sl;
+            return CART_OK;
+        }
+    }
+    *grow = 0;
+    if (stepping)  // a plan is made anyway: with a page ahead for every cache (if there is one) it lasts 64 steps and more
+        for (int32_t i = 0; i < n_ids; ++i) {
+            Cache &c = st->caches[(size_t)ids[i]];
+            (void)take_pages(ctx, st, c, (int64_t)c.len[(size_t)layer] + kTileTokens);
+        }
+    Slot *sl = nullptr;
+    cart_status r = free_slot(ctx, st, &sl);
+    if (r != CART_OK) return r;
+    const Q8Layout &lay = st->lay;
+    uint32_t *list = reinterpret_cast<uint32_t *>(sl->host + lay.pages_off);
+    uint32_t n_listed = 0;
+    ++st->list_stamp;
+    auto &segs = st->seg_tmp;
+    auto &sb = st->seg_begin_tmp;
+    segs.clear();
+    sb.assign(1, 0);
+    sl->bases.clear();
+    auto push = [&](Cache &c, int32_t n_tok, uint32_t flags) {
+        if (n_tok <= 0) return;
+        cart_plan_seg sg;
+        sg.k_row = c.list_base;
+        sg.v_row = 0;
+        sg.head_stride = 1;
+        sg.layer_stride = (uint32_t)Hkv;
+        sg.n_tok = (uint32_t)n_tok;
+        sg.flags = flags | CART_SEG_PAGED;
+        segs.push_back(sg);
+    };
+    int32_t n_rows = 0;
+    for (int32_t i = 0; i < n_ids; ++i) {
+        Cache &c = st->caches[(size_t)ids[i]];
+        bool room = list_pages(st, c, list, &n_listed);
+        for (int32_t q : c.parts) room = room && list_pages(st, st->caches[(size_t)q], list, &n_listed);
+        if (!room) return ctx_fail(ctx, CART_ERR_CAPACITY, "q8 attention: the batch names more than %d pages", lay.pages_cap);
+        sl->bases.push_back(c.list_base);
+        const int32_t m = n_new ? n_new[i] : 1, len = c.len[(size_t)layer];
+        for (int32_t r2 = 0; r2 < m; ++r2) {
+            for (int32_t q : c.parts) push(st->caches[(size_t)q], st->caches[(size_t)q].len[(size_t)layer], 0);
+            push(c, len - (m - 1 - r2), CART_SEG_SUFFIX);
+            sb.push_back((int32_t)segs.size());
+            ++n_rows;
+        }
+    }
+    cart_plan_out po{};
+    po.items = reinterpret_cast<cart_work_item *>(sl->host + lay.items_off);
+    po.items_cap = lay.items_cap;
+    po.cta_begin = reinterpret_cast<uint32_t *>(sl->host);
+    po.merges = reinterpret_cast<cart_merge_item *>(sl->host + lay.merges_off);
+    po.merges_cap = lay.merges_cap;
+    po.slots_cap = lay.slots_cap;
+    po.piece_cost = cv.piece_cost;
+    r = cart_plan_build_shared(segs.data(), sb.data(), n_rows, Hkv, cv.group, std::min(cv.n_cta, kQ8MaxCta), kTileTokens, 0,
+                               kShareTileTokens, &po);
+    if (r != CART_OK) return ctx_fail(ctx, r, "q8 attention: planning failed (%s)", cart_status_string(r));
+    sl->n_items = po.n_items;
+    sl->n_merges = po.n_merges;
+    sl->n_cta_used = po.n_cta_used;
+    Q8_CUDA(ctx, cudaMemcpyAsync(sl->dev, sl->host, lay.items_off + (uint64_t)po.n_items * sizeof(cart_work_item),
+                                 cudaMemcpyHostToDevice, s));
+    use_slot(st, sl, s);
+    Q8_CUDA(ctx, cudaMemcpyAsync(sl->dev + lay.pages_off, sl->host + lay.pages_off, (uint64_t)n_listed * 4, cudaMemcpyHostToDevice, s));
+    sl->key = key;
+    sl->lens = lens;
+    sl->epoch = st->epoch;
+    sl->kind = decode ? kDecode : kMessage;
+    *out = sl;
+    return CART_OK;
+}
+
+cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t layer, int32_t format, const void *q, void *out, float *lse,
+                             cudaStream_t s)
+{
+    const CtxView cv = ctx_view(ctx);
+    Q8State *st = *cv.q8;
+    const Q8Layout &lay = st->lay;
+    Q8StreamParams p;
+    p.cta_begin = reinterpret_cast<const uint32_t *>(sl->dev);
+    p.items = reinterpret_cast<const cart_work_item *>(sl->dev + lay.items_off);
+    p.pages = reinterpret_cast<const uint32_t *>(sl->dev + lay.pages_off);
+    p.arena = static_cast<const uint8_t *>(cv.cfg->arena);
+    p.q = q;
+    p.out = out;
+    p.lse = lse;
+    p.part_o = reinterpret_cast<float *>(st->base + lay.part_o_off);
+    p.part_lse2 = reinterpret_cast<float *>(st->base + lay.part_lse_off);
+    p.merges = reinterpret_cast<const cart_merge_item *>(sl->dev + lay.merges_off);
+    const bool merge_after = sl->n_merges > cv.n_cta;
+    p.tickets = merge_after ? nullptr : reinterpret_cast<uint32_t *>(st->base);
+    p.status = cv.status;
+    p.layer = layer;
+    p.group = cv.group;
+    p.scale_log2 = cv.scale * 1.4426950408889634f;
+    p.grow = (uint32_t)grow;
+    use_slot(st, sl, s);
+    Q8_CUDA(ctx, q8_launch_stream(p, format, sl->n_cta_used, s));
+    ++*cv.launches;
+    if (merge_after) {
+        MergeParams mp;
+        mp.merges = p.merges;
+        mp.part_o = p.part_o;
+        mp.part_lse2 = p.part_lse2;
+        mp.out = out;
+        mp.lse = lse;
+        mp.group = cv.group;
+        Q8_CUDA(ctx, launch_merge(mp, sl->n_merges, s));
+        ++*cv.launches;
+    }
+    return CART_OK;
+}
+
+// No exception leaves a C entry point (the only ones here are failed host allocations).
+template <class F>
+cart_status guarded(cart_ctx *ctx, F body)
+{
+    try {
+        return body();
+    } catch (...) {
+        return ctx ? ctx_fail(ctx, CART_ERR_OOM, "q8: out of host memory") : CART_ERR_OOM;
+    }
+}
+
+// Puts lengths and pages of a batch back as they were, unless the call has come through.
+struct Undo {
+    cart_ctx *ctx;
+    int32_t layer;
+    const cart_q8 *ids;
+    std::vector<size_t> pages;
+    std::vector<int32_t> lens;
+    bool active = true;
+    ~Undo()
+    {
+        if (!active) return;
+        Q8State *st = *ctx_view(ctx).q8;
+        for (size_t i = 0; i < pages.size(); ++i) drop_pages(ctx, st, st->caches[(size_t)ids[i]], pages[i]);
+        for (size_t i = 0; i < lens.size(); ++i) st->caches[(size_t)ids[i]].len[(size_t)layer] = lens[i];
+    }
+};
+
+cart_status check_tensors(cart_ctx *ctx, const void *q, const void *out, const float *lse, const char *what)
+{
+    if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u))
+        return ctx_fail(ctx, CART_ERR_INVALID_ARG, "%s: null/misaligned pointer", what);
+    return CART_OK;
+}
+
+}  // namespace
+}  // namespace cart
+
+using namespace cart;
+
+extern "C" {
+
+cart_status cart_q8_scratch_bytes(const cart_config *cfg, uint64_t *out_bytes)
+{
+    if (!out_bytes) return CART_ERR_INVALID_ARG;
+    const cart_status r = check(cfg);
+    if (r != CART_OK) return r;
+    *out_bytes = q8_layout(*cfg).total;
+    return CART_OK;
+}
+
+cart_status cart_q8_cache_bytes(const cart_config *cfg, int32_t n_tokens, uint64_t *out_bytes)
+{
+    if (!out_bytes || n_tokens < 0) return CART_ERR_INVALID_ARG;
+    const cart_status r = check(cfg);
+    if (r != CART_OK) return r;
+    *out_bytes = ((uint64_t)n_tokens + kTileTokens - 1) / kTileTokens * page_bytes(*cfg);
+    return CART_OK;
+}
+
+cart_status cart_q8_open(cart_ctx *ctx, int32_t format, const cart_q8 *parts, int32_t n_parts, int32_t capacity, cart_q8 *out)
+{
+    if (!ctx) return CART_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> cart_status {
+        if (!out || (format != CART_Q8_INT8 && format != CART_Q8_E4M3) || n_parts < 0 || (n_parts > 0 && !parts) || capacity < 0 ||
+            capacity > INT32_MAX - kTileTokens)
+            return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_open: bad argument");
+        const CtxView cv = ctx_view(ctx);
+        std::vector<int32_t> flat;
+        for (int32_t i = 0; i < n_parts; ++i) {
+            const Cache *c = get(ctx, parts[i]);
+            if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_open: part %d is not an open cache", i);
+            if (c->format != format) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_open: part %d is of another format", i);
+            flat.insert(flat.end(), c->parts.begin(), c->parts.end());
+            flat.push_back(parts[i]);
+        }
+        if ((int64_t)flat.size() > cv.cfg->max_parts)
+            return ctx_fail(ctx, CART_ERR_CAPACITY, "q8_open: %d parts exceed max_parts = %d", (int)flat.size(), cv.cfg->max_parts);
+        OnDevice dev(cv.cfg->device);
+        const cart_status r = make_state(ctx);
+        if (r != CART_OK) return r;
+        Q8State *st = *cv.q8;
+        size_t id = 0;
+        while (id < st->caches.size() && st->caches[id].live) ++id;
+        if (id == st->caches.size()) st->caches.emplace_back();
+        Cache &c = st->caches[id];
+        c = Cache();
+        if (!take_pages(ctx, st, c, capacity)) {
+            drop_pages(ctx, st, c, 0);
+            return ctx_fail(ctx, CART_ERR_OOM, "q8_open: the arena has no room for %d tokens", capacity);
+        }
+        c.live = true;
+        c.format = format;
+        c.parts = flat;
+        c.len.assign((size_t)cv.cfg->n_layers, 0);
+        for (int32_t q : flat) ++st->caches[(size_t)q].refs;
+        ++st->epoch;
+        *out = (cart_q8)id;
+        return CART_OK;
+    });
+}
+
+cart_status cart_q8_close(cart_ctx *ctx, cart_q8 id)
+{
+    if (!ctx) return CART_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> cart_status {
+        Cache *c = get(ctx, id);
+        if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_close: not an open cache");
+        if (c->refs > 0) return ctx_fail(ctx, CART_ERR_IN_USE, "q8_close: %d caches stand behind it", c->refs);
+        Q8State *st = *ctx_view(ctx).q8;
+        for (int32_t q : c->parts) --st->caches[(size_t)q].refs;
+        drop_pages(ctx, st, *c, 0);
+        *c = Cache();
+        ++st->epoch;
+        return CART_OK;
+    });
+}
+
+cart_status cart_q8_write(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t n_ids, const int32_t *first, const int32_t *n_tokens,
+                          const void *k, const void *v, int64_t token_stride, int64_t head_stride, void *stream)
+{
+    if (!ctx) return CART_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> cart_status {
+        if (!n_tokens) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_write: null n_tokens");
+        if (token_stride < 0 || head_stride < 0 || token_stride % 8 != 0 || head_stride % 8 != 0)
+            return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_write: strides must be multiples of 8 elements, not negative");
+        const CtxView cv = ctx_view(ctx);
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        OnDevice dev(cv.cfg->device);
+        cart_status r = not_capturing(ctx, s, "q8_write");
+        if (r != CART_OK) return r;
+        std::vector<int32_t> at;
+        Undo undo{ctx, layer, ids, {}, {}};
+        int32_t format = 0;
+        int64_t total = 0;
+        for (int32_t i = 0; i < n_ids && ids; ++i) total += n_tokens[i] > 0 ? n_tokens[i] : 0;
+        if (total > 0 && (!aligned16(k) || !aligned16(v))) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_write: null/misaligned pointer");
+        r = prepare_write(ctx, layer, ids, n_ids, first, n_tokens, &at, &undo.pages, &format, &total, "q8_write");
+        if (r != CART_OK) return r;
+        Q8State *st = *cv.q8;
+        if (total > 0) {
+            Slot *sl = nullptr;
+            r = list_slot(ctx, ids, n_ids, s, &sl);
+            if (r != CART_OK) return r;
+            use_slot(st, sl, s);
+            undo.active = false;
+            r = launch_copy(ctx, true, sl, layer, format, n_ids, at.data(), n_tokens, k, v, token_stride, head_stride, s);
+            if (r != CART_OK) return r;
+        }
+        undo.active = false;
+        for (int32_t i = 0; i < n_ids; ++i) st->caches[(size_t)ids[i]].len[(size_t)layer] = at[(size_t)i] + n_tokens[i];
+        return CART_OK;
+    });
+}
+
+cart_status cart_q8_read(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t n_ids, const int32_t *first, const int32_t *n_tokens,
+                         void *k, void *v, void *stream)
+{
+    if (!ctx) return CART_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> cart_status {
+        if (!ids || n_ids < 1 || !first || !n_tokens) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_read: empty batch or null array");
+        const CtxView cv = ctx_view(ctx);
+        if (layer < 0 || layer >= cv.cfg->n_layers) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_read: layer out of range");
+        int64_t total = 0;
+        int32_t format = 0;
+        for (int32_t i = 0; i < n_ids; ++i) {
+            const Cache *c = get(ctx, ids[i]);
+            if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_read: ids[%d] is not an open cache", i);
+            if (i == 0) format = c->format;
+            if (c->format != format) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_read: the caches are of different formats");
+            if (first[i] < 0 || n_tokens[i] < 0 || (int64_t)first[i] + n_tokens[i] > c->len[(size_t)layer])
+                return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_read: cache %d holds %d tokens: cannot read %d from %d on", i,
+                                c->len[(size_t)layer], n_tokens[i], first[i]);
+            total += n_tokens[i];
+        }
+        if (total > INT32_MAX) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_read: too many tokens");
+        if (total == 0) return CART_OK;
+        if (!aligned16(k) || !aligned16(v)) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_read: null/misaligned pointer");
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        OnDevice dev(cv.cfg->device);
+        cart_status r = not_capturing(ctx, s, "q8_read");
+        if (r != CART_OK) return r;
+        Slot *sl = nullptr;
+        r = list_slot(ctx, ids, n_ids, s, &sl);
+        if (r != CART_OK) return r;
+        use_slot(*cv.q8, sl, s);
+        return launch_copy(ctx, false, sl, layer, format, n_ids, first, n_tokens, k, v, (int64_t)cv.cfg->n_kv_heads * kHeadDim, kHeadDim, s);
+    });
+}
+
+cart_status cart_q8_attention(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t n_ids, const int32_t *n_new, const void *q,
+                              void *out, float *lse, void *stream)
+{
+    if (!ctx) return CART_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> cart_status {
+        if (!ids || n_ids < 1) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_attention: empty batch");
+        const CtxView cv = ctx_view(ctx);
+        if (layer < 0 || layer >= cv.cfg->n_layers) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_attention: layer out of range");
+        int64_t rows = 0;
+        int32_t format = 0;
+        for (int32_t i = 0; i < n_ids; ++i) {
+            const Cache *c = get(ctx, ids[i]);
+            if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_attention: ids[%d] is not an open cache", i);
+            if (i == 0) format = c->format;
+            if (c->format != format) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_attention: the caches are of different formats");
+            const int32_t m = n_new ? n_new[i] : 1, len = c->len[(size_t)layer];
+            if (m < 0 || (m > 1 && m > len))
+                return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_attention: cache %d holds %d tokens, n_new is %d", i, len, m);
+            if (m == 0) continue;
+            int64_t sees = len;
+            for (int32_t x : c->parts) sees += (*cv.q8)->caches[(size_t)x].len[(size_t)layer];
+            if (sees == 0) return ctx_fail(ctx, CART_ERR_EMPTY, "q8_attention: ids[%d] has no token in layer %d", i, layer);
+            rows += m;
+        }
+        if (rows == 0) return CART_OK;
+        if (rows > cv.cfg->max_requests)
+            return ctx_fail(ctx, CART_ERR_CAPACITY, "q8_attention: %lld rows exceed max_requests %d", (long long)rows, cv.cfg->max_requests);
+        cart_status r = check_tensors(ctx, q, out, lse, "q8_attention");
+        if (r != CART_OK) return r;
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        OnDevice dev(cv.cfg->device);
+        r = not_capturing(ctx, s, "q8_attention");
+        if (r != CART_OK) return r;
+        Slot *sl = nullptr;
+        int32_t grow = 0;
+        r = plan_slot(ctx, layer, ids, n_ids, n_new, false, s, &sl, &grow);
+        if (r != CART_OK) return r;
+        return launch_attention(ctx, sl, grow, layer, format, q, out, lse, s);
+    });
+}
+
+cart_status cart_q8_decode_step(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t n_ids, const int32_t *first, const void *k_new,
+                                const void *v_new, const void *q, void *out, float *lse, void *stream)
+{
+    if (!ctx) return CART_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> cart_status {
+        if (!aligned16(k_new) || !aligned16(v_new)) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_decode_step: null/misaligned pointer");
+        cart_status r = check_tensors(ctx, q, out, lse, "q8_decode_step");
+        if (r != CART_OK) return r;
+        const CtxView cv = ctx_view(ctx);
+        if (n_ids > cv.cfg->max_requests)
+            return ctx_fail(ctx, CART_ERR_CAPACITY, "q8_decode_step: batch %d exceeds max_requests %d", n_ids, cv.cfg->max_requests);
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        OnDevice dev(cv.cfg->device);
+        r = not_capturing(ctx, s, "q8_decode_step");
+        if (r != CART_OK) return r;
+        std::vector<int32_t> at;
+        Undo undo{ctx, layer, ids, {}, {}};
+        int32_t format = 0;
+        int64_t total = 0;
+        r = prepare_write(ctx, layer, ids, n_ids, first, nullptr, &at, &undo.pages, &format, &total, "q8_decode_step");
+        if (r != CART_OK) return r;
+        Q8State *st = *cv.q8;
+        std::vector<int32_t> ones((size_t)n_ids, 1);
+        // the plan must see the new tokens; they are taken back if nothing was launched
+        for (int32_t i = 0; i < n_ids; ++i) undo.lens.push_back(st->caches[(size_t)ids[i]].len[(size_t)layer]);
+        for (int32_t i = 0; i < n_ids; ++i) st->caches[(size_t)ids[i]].len[(size_t)layer] = at[(size_t)i] + 1;
+        Slot *sl = nullptr;
+        int32_t grow = 0;
+        r = plan_slot(ctx, layer, ids, n_ids, nullptr, true, s, &sl, &grow);
+        if (r != CART_OK) return r;
+        undo.active = false;
+        use_slot(st, sl, s);
+        r = launch_copy(ctx, true, sl, layer, format, n_ids, at.data(), ones.data(), k_new, v_new, (int64_t)cv.cfg->n_kv_heads * kHeadDim,
+                        kHeadDim, s);
+        if (r != CART_OK) return r;
+        return launch_attention(ctx, sl, grow, layer, format, q, out, lse, s);
+    });
+}
+
+cart_status cart_q8_from_cartridge(cart_ctx *ctx, cart_id cartridge, int32_t format, void *stream, cart_q8 *out)
+{
+    if (!ctx) return CART_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> cart_status {
+        if (!out) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_from_cartridge: null out");
+        const CtxView cv = ctx_view(ctx);
+        uint64_t k_row = 0, v_row = 0;
+        int32_t p = 0;
+        cart_status r = ctx_cartridge(ctx, cartridge, &k_row, &v_row, &p);
+        if (r != CART_OK) return ctx_fail(ctx, r, "q8_from_cartridge: not a registered Cartridge in the arena");
+        cudaStream_t s = static_cast<cudaStream_t>(stream);
+        {
+            OnDevice dev(cv.cfg->device);
+            r = not_capturing(ctx, s, "q8_from_cartridge");
+            if (r != CART_OK) return r;
+        }
+        cart_q8 id = -1;
+        r = cart_q8_open(ctx, format, nullptr, 0, p, &id);
+        if (r != CART_OK) return r;
+        // [n_layers][n_kv_heads][p][128] in the arena
+        const int Hkv = cv.cfg->n_kv_heads;
+        uint8_t *arena = static_cast<uint8_t *>(cv.cfg->arena);
+        for (int32_t l = 0; l < cv.cfg->n_layers && r == CART_OK; ++l) {
+            const uint64_t off = (uint64_t)l * Hkv * (uint64_t)p;
+            r = cart_q8_write(ctx, l, &id, 1, nullptr, &p, arena + (k_row + off) * kRowBytes, arena + (v_row + off) * kRowBytes, kHeadDim,
+                              (int64_t)p * kHeadDim, stream);
+        }
+        if (r != CART_OK) {
+            (void)cart_q8_close(ctx, id);
+            return r;
+        }
+        *out = id;
+        return CART_OK;
+    });
+}
+
+cart_status cart_q8_len(cart_ctx *ctx, cart_q8 id, int32_t layer, int32_t *own, int64_t *total)
+{
+    if (!ctx) return CART_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> cart_status {
+        const CtxView cv = ctx_view(ctx);
+        const Cache *c = get(ctx, id);
+        if (!c || layer < 0 || layer >= cv.cfg->n_layers) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_len: bad handle");
+        if (own) *own = c->len[(size_t)layer];
+        if (total) {
+            *total = c->len[(size_t)layer];
+            for (int32_t x : c->parts) *total += (*cv.q8)->caches[(size_t)x].len[(size_t)layer];
+        }
+        return CART_OK;
+    });
+}
+
+}  // extern "C"

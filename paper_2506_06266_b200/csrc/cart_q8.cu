@@ -1,0 +1,756 @@
+// Caches in 8 bits for sm_100a: quantising tokens as they are written, reading them back, and attention that streams a
+// cache (one to eight query heads per KV head).  The format is in include/cart_q8.h, the layout in cart_q8_internal.h.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "cart_device.cuh"
+#include "cart_q8_internal.h"
+
+namespace cart {
+namespace {
+
+// ---- codes ------------------------------------------------------------------------------------------
+
+// 2^x for a whole number x of -126 .. 127
+__device__ __forceinline__ float exp2_int(int x) { return __uint_as_float((uint32_t)(x + 127) << 23); }
+
+// the stored scale byte for a block whose largest magnitude has the bf16 bits `a` (sign clear)
+template <int kFmt>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t a)
+{
+    if (a >= 0x7F80u) return kQ8NoScale;              // a NaN or an infinity
+    const int x = (int)(a >> 7) - 127;                // a = 2^x * (1 + m / 128) (subnormal: far below the smallest scale)
+    const uint32_t m = a & 0x7Fu;
+    // int8: a <= 127 * 2^e, and 127 = 2^6 * (1 + 126/128); e4m3: 448 = 2^8 * (1 + 96/128)
+    const int e = kFmt == CART_Q8_INT8 ? x - 6 + (m > 126u ? 1 : 0) : x - 8 + (m > 96u ? 1 : 0);
+    return (uint32_t)(max(e, kQ8MinExp) + 127);
+}
+
+// four values, already scaled, -> four stored codes (first value in the low byte)
+template <int kFmt>
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d)
+{
+    if (kFmt == CART_Q8_INT8) {
+        // (no value leaves -127 .. 127: the scale is chosen so; conversion rounds half to even)
+        const uint32_t x = (uint32_t)(__float2int_rn(a) + 128), y = (uint32_t)(__float2int_rn(b) + 128);
+        const uint32_t z = (uint32_t)(__float2int_rn(c) + 128), w = (uint32_t)(__float2int_rn(d) + 128);
+        return x | (y << 8) | (z << 16) | (w << 24);
+    }
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+    return lo | (hi << 16);
+}
+
+// four stored codes -> two pairs of fp16 (exact)
+template <int kFmt>
+__device__ __forceinline__ void decode4(uint32_t r, uint32_t &lo, uint32_t &hi)
+{
+    if (kFmt == CART_Q8_INT8) {
+        // a byte u under the high byte 0x64 is the fp16 number 1024 + u; less 1024 + 128 it is the code
+        const uint32_t a = __byte_perm(r, 0x64646464u, 0x4140), b = __byte_perm(r, 0x64646464u, 0x4342);
+        const __half2 off = __half2half2(__ushort_as_half((unsigned short)0x6480));
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), off), y = __hsub2(*reinterpret_cast<const __half2 *>(&b), off);
+        lo = *reinterpret_cast<const uint32_t *>(&x);
+        hi = *reinterpret_cast<const uint32_t *>(&y);
+    } else {
+        asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %2;\ncvt.rn.f16x2.e4m3x2 %0, l;\ncvt.rn.f16x2.e4m3x2 %1, h;\n}\n"
+            : "=r"(lo), "=r"(hi)
+            : "r"(r));
+    }
+}
+template <int kFmt>
+__device__ __forceinline__ void decode4(uint32_t r, float (&f)[4])
+{
+    uint32_t lo, hi;
+    decode4<kFmt>(r, lo, hi);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&lo)), b = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
+    f[0] = a.x;
+    f[1] = a.y;
+    f[2] = b.x;
+    f[3] = b.y;
+}
+
+// ---- write and read ------------------------------------------------------------------------------------
+// One thread block per block of 16 tokens, one warp at a time per (KV head, keys or values).  Both kernels move a few KB
+// per warp in 16-byte accesses and do little arithmetic: HBM bounds them for long ranges, the launch for short ones.
+
+constexpr int kCopyThreads = 256;
+
+// the entry that owns block number `task` of the call
+__device__ __forceinline__ Q8Entry find_entry(const Q8CopyParams &p, uint32_t task)
+{
+    int lo = 0, hi = p.n_entries - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.e[mid].task_begin <= task) lo = mid;
+        else hi = mid - 1;
+    }
+    return p.e[lo];
+}
+
+// Lane l of a warp that walks a block row by row holds the dims 8 (l % 16) .. + 7 of the tokens 2 i + l / 16.  In the
+// stored order of values a word holds one dim of the tokens 2i, 2i + 1, 2i + 8, 2i + 9, so lanes l and l ^ 16 trade half
+// of their dims: the lower lane ends up with the words of the dims 0 .. 3 of its eight, the upper one with 4 .. 7.
+// a: codes of token 2i (+1), b: of token 2i + 8 (+1), dims 0 .. 3 in [0].
+__device__ __forceinline__ void rows_to_words(const uint32_t (&a)[2], const uint32_t (&b)[2], bool upper, uint32_t (&w)[4])
+{
+    const uint32_t keep_a = upper ? a[1] : a[0], give_a = upper ? a[0] : a[1];
+    const uint32_t keep_b = upper ? b[1] : b[0], give_b = upper ? b[0] : b[1];
+    const uint32_t got_a = __shfl_xor_sync(0xffffffffu, give_a, 16), got_b = __shfl_xor_sync(0xffffffffu, give_b, 16);
+    const uint32_t a0 = upper ? got_a : keep_a, a1 = upper ? keep_a : got_a;   // tokens 2i, 2i + 1
+    const uint32_t b0 = upper ? got_b : keep_b, b1 = upper ? keep_b : got_b;   // tokens 2i + 8, 2i + 9
+    const uint32_t a_lo = __byte_perm(a0, a1, 0x5140), a_hi = __byte_perm(a0, a1, 0x7362);  // dims 0, 1 | 2, 3
+    const uint32_t b_lo = __byte_perm(b0, b1, 0x5140), b_hi = __byte_perm(b0, b1, 0x7362);
+    w[0] = __byte_perm(a_lo, b_lo, 0x5410);
+    w[1] = __byte_perm(a_lo, b_lo, 0x7632);
+    w[2] = __byte_perm(a_hi, b_hi, 0x5410);
+    w[3] = __byte_perm(a_hi, b_hi, 0x7632);
+}
+// The inverse.
+__device__ __forceinline__ void words_to_rows(const uint32_t (&w)[4], bool upper, uint32_t (&a)[2], uint32_t (&b)[2])
+{
+    const uint32_t a_lo = __byte_perm(w[0], w[1], 0x5410), b_lo = __byte_perm(w[0], w[1], 0x7632);
+    const uint32_t a_hi = __byte_perm(w[2], w[3], 0x5410), b_hi = __byte_perm(w[2], w[3], 0x7632);
+    const uint32_t a0 = __byte_perm(a_lo, a_hi, 0x6420), a1 = __byte_perm(a_lo, a_hi, 0x7531);
+    const uint32_t b0 = __byte_perm(b_lo, b_hi, 0x6420), b1 = __byte_perm(b_lo, b_hi, 0x7531);
+    const uint32_t keep_a = upper ? a1 : a0, give_a = upper ? a0 : a1;
+    const uint32_t keep_b = upper ? b1 : b0, give_b = upper ? b0 : b1;
+    const uint32_t got_a = __shfl_xor_sync(0xffffffffu, give_a, 16), got_b = __shfl_xor_sync(0xffffffffu, give_b, 16);
+    a[0] = upper ? got_a : keep_a;
+    a[1] = upper ? keep_a : got_a;
+    b[0] = upper ? got_b : keep_b;
+    b[1] = upper ? keep_b : got_b;
+}
+
+template <int kFmt>
+__global__ void __launch_bounds__(kCopyThreads) cart_q8_write_kernel(const __grid_constant__ Q8CopyParams p)
+{
+    __shared__ __align__(16) uint8_t stage[kCopyThreads / 32][kQ8ValueOff];
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Q8Entry e = find_entry(p, blockIdx.x);
+    const uint32_t b = e.first / kQ8Block + (blockIdx.x - e.task_begin);
+    const uint32_t page = __ldg(p.pages + e.list + b / (kTileTokens / kQ8Block));
+    const uint32_t tok0 = b * kQ8Block, end = e.first + e.n;
+    const uint32_t kept = e.first > tok0 ? e.first - tok0 : 0u;  // tokens that the block holds already
+    pdl_wait();  // k and v, and the codes held already, come from the kernels before
+    uint8_t *st = stage[warp];
+    const bool upper = lane >= 16;
+    const uint32_t c16 = (uint32_t)lane & 15u;                   // dims 8 c16 .. 8 c16 + 7
+    for (int u = warp; u < 2 * p.n_kv_heads; u += kCopyThreads / 32) {
+        const int h = u >> 1;
+        const bool is_v = (u & 1) != 0;
+        uint8_t *blk = p.arena + (size_t)page * kRowBytes +
+                       ((size_t)(p.layer * p.n_kv_heads + h) * (kTileTokens / kQ8Block) + b % (kTileTokens / kQ8Block)) * kQ8BlockBytes;
+        uint4 *codes = reinterpret_cast<uint4 *>(blk + (is_v ? kQ8ValueOff : 0u));
+        uint8_t *scale = blk + kQ8ScaleOff + (is_v ? 1 : 0);
+        const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(is_v ? p.v : p.k) + (int64_t)h * p.head_stride + 8 * c16;
+        uint4 x[8], old[4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t tok = tok0 + 2u * i + (upper ? 1u : 0u);
+            x[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (tok >= e.first && tok < end)
+                x[i] = *reinterpret_cast<const uint4 *>(src + (int64_t)(e.src + (tok - e.first)) * p.token_stride);
+        }
+        uint32_t eb_old = 0u;
+        if (kept > 0u) {
+            eb_old = *scale;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) old[c] = codes[c * 32 + lane];
+        }
+        uint32_t big = 0u;  // two 16-bit maxima of the magnitudes' bits
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            big = __vmaxu2(big, __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu)));
+        }
+        big = max(big & 0xFFFFu, big >> 16);
+        big = __reduce_max_sync(0xffffffffu, big);
+        const uint32_t eb = max(scale_byte<kFmt>(big), eb_old);  // (no scale, 255, is the largest of all)
+        // 2^-e; a block without a scale holds zeros
+        const float down = eb == kQ8NoScale ? 0.f : exp2_int(127 - (int)eb);
+        uint32_t code[8][2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f[2 * j] = __uint_as_float(w[j] << 16) * down;
+                f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u) * down;
+            }
+            if (eb == kQ8NoScale) {  // (0 * NaN is not 0)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = 0.f;
+            }
+            code[i][0] = encode4<kFmt>(f[0], f[1], f[2], f[3]);
+            code[i][1] = encode4<kFmt>(f[4], f[5], f[6], f[7]);
+        }
+        // to the stored order, through shared memory
+        __syncwarp();
+        if (is_v) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t w[4];
+                rows_to_words(code[i], code[i + 4], upper, w);
+                const uint32_t chunk = c16 >> 2, word = 2u * ((c16 >> 1) & 1u) + (c16 & 1u), dg = upper ? 4u : 0u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<uint32_t *>(st + chunk * 512u + ((dg + j) * 4u + i) * 16u + word * 4u) = w[j];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t row = 2u * i + (upper ? 1u : 0u);
+                const uint32_t chunk = c16 >> 2, word = 2u * ((c16 >> 1) & 1u) + (row >> 3), l0 = (row & 7u) * 4u + 2u * (c16 & 1u);
+                *reinterpret_cast<uint32_t *>(st + chunk * 512u + l0 * 16u + word * 4u) = code[i][0];
+                *reinterpret_cast<uint32_t *>(st + chunk * 512u + (l0 + 1u) * 16u + word * 4u) = code[i][1];
+            }
+        }
+        __syncwarp();
+        uint4 mine[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) mine[c] = *reinterpret_cast<const uint4 *>(st + c * 512 + lane * 16);
+        if (kept > 0u) {
+            // codes held already stay, rounded once more if the scale has grown
+            const uint32_t g = (uint32_t)lane >> 2, t = (uint32_t)lane & 3u;
+            const int grown = (int)eb - (int)eb_old;
+            const float f = exp2_int(-min(grown, 30));  // (beyond that every code rounds to zero)
+            uint32_t mask[2];                            // bytes of the even and odd words that are kept
+            if (is_v) {
+                uint32_t m = 0u;
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j)
+                    if ((j >> 1) * 8u + 2u * t + (j & 1u) < kept) m |= 0xFFu << (8u * j);
+                mask[0] = mask[1] = m;
+            } else {
+                mask[0] = g < kept ? 0xFFFFFFFFu : 0u;
+                mask[1] = g + 8u < kept ? 0xFFFFFFFFu : 0u;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t o[4] = {old[c].x, old[c].y, old[c].z, old[c].w}, n[4] = {mine[c].x, mine[c].y, mine[c].z, mine[c].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (grown > 0 && eb != kQ8NoScale) {
+                        float v[4];
+                        decode4<kFmt>(o[j], v);
+                        o[j] = encode4<kFmt>(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+                    }
+                    n[j] = (o[j] & mask[j & 1]) | (n[j] & ~mask[j & 1]);
+                }
+                mine[c] = make_uint4(n[0], n[1], n[2], n[3]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) codes[c * 32 + lane] = mine[c];
+        if (lane == 0) *scale = (uint8_t)eb;
+    }
+    asm volatile("fence.proxy.async;" ::: "memory");  // the attention kernel's bulk copies read what was written here
+}
+
+template <int kFmt>
+__global__ void __launch_bounds__(kCopyThreads) cart_q8_read_kernel(const __grid_constant__ Q8CopyParams p)
+{
+    __shared__ __align__(16) uint8_t stage[kCopyThreads / 32][kQ8ValueOff];
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Q8Entry e = find_entry(p, blockIdx.x);
+    const uint32_t b = e.first / kQ8Block + (blockIdx.x - e.task_begin);
+    const uint32_t page = __ldg(p.pages + e.list + b / (kTileTokens / kQ8Block));
+    const uint32_t tok0 = b * kQ8Block, end = e.first + e.n;
+    pdl_wait();
+    uint8_t *st = stage[warp];
+    const bool upper = lane >= 16;
+    const uint32_t c16 = (uint32_t)lane & 15u;
+    for (int u = warp; u < 2 * p.n_kv_heads; u += kCopyThreads / 32) {
+        const int h = u >> 1;
+        const bool is_v = (u & 1) != 0;
+        const uint8_t *blk = p.arena + (size_t)page * kRowBytes +
+                             ((size_t)(p.layer * p.n_kv_heads + h) * (kTileTokens / kQ8Block) + b % (kTileTokens / kQ8Block)) * kQ8BlockBytes;
+        const uint4 *codes = reinterpret_cast<const uint4 *>(blk + (is_v ? kQ8ValueOff : 0u));
+        const uint32_t eb = blk[kQ8ScaleOff + (is_v ? 1 : 0)];
+        uint4 x[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] = codes[c * 32 + lane];
+        const float up = eb == kQ8NoScale ? __uint_as_float(0x7FC00000u) : exp2_int((int)eb - 127);
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(st + c * 512 + lane * 16) = x[c];
+        __syncwarp();
+        uint32_t code[8][2];
+        const uint32_t chunk = c16 >> 2;
+        if (is_v) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t word = 2u * ((c16 >> 1) & 1u) + (c16 & 1u), dg = upper ? 4u : 0u;
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = *reinterpret_cast<const uint32_t *>(st + chunk * 512u + ((dg + j) * 4u + i) * 16u + word * 4u);
+                words_to_rows(w, upper, code[i], code[i + 4]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t row = 2u * i + (upper ? 1u : 0u);
+                const uint32_t word = 2u * ((c16 >> 1) & 1u) + (row >> 3), l0 = (row & 7u) * 4u + 2u * (c16 & 1u);
+                code[i][0] = *reinterpret_cast<const uint32_t *>(st + chunk * 512u + l0 * 16u + word * 4u);
+                code[i][1] = *reinterpret_cast<const uint32_t *>(st + chunk * 512u + (l0 + 1u) * 16u + word * 4u);
+            }
+        }
+        __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(const_cast<void *>(is_v ? p.v : p.k)) + (int64_t)h * p.head_stride + 8 * c16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t tok = tok0 + 2u * i + (upper ? 1u : 0u);
+            if (tok < e.first || tok >= end) continue;
+            float f[4], g[4];
+            decode4<kFmt>(code[i][0], f);
+            decode4<kFmt>(code[i][1], g);
+            *reinterpret_cast<uint4 *>(dst + (int64_t)(e.src + (tok - e.first)) * p.token_stride) =
+                make_uint4(pack_bf16(f[0] * up, f[1] * up), pack_bf16(f[2] * up, f[3] * up), pack_bf16(g[0] * up, g[1] * up),
+                           pack_bf16(g[2] * up, g[3] * up));
+        }
+    }
+}
+
+// ---- attention that streams a cache ----------------------------------------------------------------------
+// The work list is the planner's (cart_plan.h): block c runs the items cta_begin[c] .. cta_begin[c + 1] - 1, each a run
+// of pages of one (query row, KV head).  Every warp is a stream of its own: of the blocks of 16 tokens that lie end to
+// end in the thread block's items, warp w takes every kWarps-th.  It copies them into a ring of its own in shared
+// memory (one bulk copy per block: keys, values and scales), and per block computes, for the G query heads (columns of
+// the products, G <= 8):
+//
+//   S^T [16 x 8] = K [16 x 128] Q^T [128 x 8]     8 products m16n8k16, codes as fp16 (exact), q as fp16 over a power of two
+//   s = S * 2^eK * scale log2(e);  m, R: running references;  l += 2^(s - m);  w = 2^(s + eV - R)
+//   O^T [128 x 8] += V^T [128 x 16] w^T [16 x 8]  8 products, codes as fp16, w as fp16
+//
+// The tokens are the long side of both products, so no row of the matrix instructions is wasted on a group of eight.
+// The values' scales join the exponent instead of multiplying codes or probabilities: w = p * 2^eV is held relative to
+// the largest such product (reference R, apart from the softmax's own reference m), so it is a number of at most 2^8
+// that fp16 holds to 2^-11 wherever it matters.  That rounding is the only one on the way besides fp32 sums; the sum l
+// is taken over unrounded numbers.  References only move when outgrown by more than 2^8 (a vote per block).
+// out = O * 2^(R - m) / l.
+constexpr int kWarps = 12;
+constexpr int kStages = 4;
+constexpr int kStreamThreads = kWarps * 32;
+constexpr float kStep = 8.f;  // how far a value may outgrow its reference (base 2)
+constexpr uint32_t kStageStride = kQ8BlockBytes;
+constexpr uint32_t kRowStride = kHeadDim + 4;  // fp32 per (warp, head) row of the combine buffer (bank spread)
+constexpr uint32_t kOffRing = 0;
+constexpr uint32_t kOffComb = kOffRing + kWarps * kStages * kStageStride;
+constexpr uint32_t kOffStat = kOffComb + (kWarps / 2) * kMaxGroup * kRowStride * 4;  // [2][warp][head]{m, l, R}
+constexpr uint32_t kOffBars = kOffStat + 2 * kWarps * kMaxGroup * 3 * 4;
+constexpr uint32_t kOffFlag = kOffBars + kWarps * kStages * 8;
+constexpr uint32_t kStreamSmem = kOffFlag + 16;
+static_assert(kStreamSmem <= 232448, "shared memory budget of one sm_100 block exceeded");
+static_assert(kOffComb % 16 == 0 && kOffBars % 8 == 0, "alignment");
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t policy)
+{
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+        "l"(src), "r"(bytes), "r"(bar), "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+
+// Walks the blocks that one warp takes from the thread block's items.
+struct Cursor {
+    uint32_t it, j, n_blk;   // item, block inside it, blocks in it
+    uint32_t at;             // (blocks of the items before) mod kWarps
+};
+
+template <int kFmt>
+__global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const Q8StreamParams p)
+{
+    extern __shared__ __align__(128) uint8_t smem[];
+    const uint32_t base = smem_u32(smem);
+    float *comb = reinterpret_cast<float *>(smem + kOffComb);
+    float *stat = reinterpret_cast<float *>(smem + kOffStat);
+    volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(smem + kOffFlag);
+    volatile uint32_t *merge_flag = abort_flag + 1;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g = lane >> 2, t = lane & 3;
+    const int G = p.group;
+    const uint32_t ring = base + kOffRing + (uint32_t)warp * kStages * kStageStride;
+    auto full = [&](uint32_t s) { return base + kOffBars + ((uint32_t)warp * kStages + s) * 8u; };
+    pdl_launch_dependents();
+    if (lane == 0) {
+        for (uint32_t s = 0; s < kStages; ++s) mbar_init(full(s), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 0) *abort_flag = 0;
+    __syncthreads();
+
+    const uint32_t item_begin = p.cta_begin[blockIdx.x], item_end = p.cta_begin[blockIdx.x + 1];
+    pdl_wait();  // the cache's last tokens, q, out and the partial slots belong to the kernels before until they are done
+    const uint64_t once = l2_evict_first_policy();
+
+    auto tokens_of = [&](const cart_work_item &w) { return w.n_tok + ((w.flags & CART_ITEM_TAIL) ? p.grow : 0u); };
+    auto first_of = [&](uint32_t at) { return ((uint32_t)warp + kWarps - at) % kWarps; };
+    // ---- the issuing side: lane 0 requests blocks in the order in which the warp will want them
+    Cursor ic{item_begin, 0u, 0u, 0u};
+    cart_work_item iw{}, iw_next{};
+    if (item_begin < item_end) {
+        iw = p.items[item_begin];
+        if (item_begin + 1 < item_end) iw_next = p.items[item_begin + 1];
+        ic.n_blk = (tokens_of(iw) + kQ8Block - 1) / kQ8Block;
+        ic.j = first_of(0u);
+    }
+    uint32_t issued = 0;       // blocks requested so far
+    uint32_t page_lane = 0;    // base row of the page of the warp's (32 c + lane)-th block of the item
+    uint32_t nth = 0;          // blocks of the item requested by this warp
+    auto issue_one = [&]() {
+        while (ic.it < item_end && ic.j >= ic.n_blk) {
+            ic.at = (ic.at + ic.n_blk) % kWarps;
+            ++ic.it;
+            iw = iw_next;
+            if (ic.it >= item_end) return;
+            if (ic.it + 1 < item_end) iw_next = p.items[ic.it + 1];
+            ic.n_blk = (tokens_of(iw) + kQ8Block - 1) / kQ8Block;
+            ic.j = first_of(ic.at);
+            nth = 0;
+        }
+        if (ic.it >= item_end) return;
+        if ((nth & 31u) == 0u) {
+            const uint32_t jj = ic.j + (uint32_t)lane * kWarps;
+            page_lane = jj < ic.n_blk ? __ldg(p.pages + iw.k_row + jj / (kTileTokens / kQ8Block)) : 0u;
+        }
+        const uint32_t page = __shfl_sync(0xffffffffu, page_lane, (int)(nth & 31u));
+        const uint32_t s = issued % kStages;
+        if (lane == 0) {
+            const uint8_t *src = p.arena + (size_t)page * kRowBytes +
+                                 ((size_t)((uint32_t)p.layer * iw.layer_stride + iw.v_row) * (kTileTokens / kQ8Block) +
+                                  ic.j % (kTileTokens / kQ8Block)) * kQ8BlockBytes;
+            mbar_expect_tx(full(s), kQ8BlockBytes);
+            bulk_load(ring + s * kStageStride, src, kQ8BlockBytes, full(s), once);
+        }
+        ++issued;
+        ++nth;
+        ic.j += kWarps;
+    };
+#pragma unroll 1
+    for (int s = 0; s < kStages; ++s) issue_one();
+
+    // ---- the computing side
+    uint32_t done = 0;            // blocks computed so far
+    uint32_t at = 0;              // as Cursor::at
+    bool alive = true;
+    uint32_t piece = 0;
+    uint32_t qb[8][2];            // Q^T fragments (head g)
+    float f0 = 0.f, f1 = 0.f;     // scale log2(e) 2^(q's exponent) of the heads 2t, 2t + 1
+    float o[8][4];                // O^T: dims 16 i + g (+ 8), heads 2t, 2t + 1
+    float m0 = 0.f, m1 = 0.f, r0 = 0.f, r1 = 0.f, l0 = 0.f, l1 = 0.f;
+    const float none = -INFINITY;
+    for (uint32_t it = item_begin; it < item_end; ++it) {
+        const cart_work_item w = p.items[it];
+        const uint32_t n_tok = tokens_of(w), n_blk = (n_tok + kQ8Block - 1) / kQ8Block;
+        if (w.flags & CART_ITEM_BEGIN) {
+            m0 = m1 = r0 = r1 = none;
+            l0 = l1 = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+            // Head g's query row, 4 consecutive dims per 16: as fp16 over a power of two that brings its largest value to
+            // 1 .. 2.  (Exact, but for values below 2^-14 of the largest, which keep an absolute error of 2^-25 of it.)
+            uint2 raw[8];
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+                raw[ks] = g < G ? __ldg(reinterpret_cast<const uint2 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) +
+                                                                        ((size_t)w.row_group * G + g) * kHeadDim + 16 * ks + 4 * t))
+                                : make_uint2(0u, 0u);
+            uint32_t big = 0u;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) big = __vmaxu2(big, __vmaxu2(raw[ks].x & 0x7FFF7FFFu, raw[ks].y & 0x7FFF7FFFu));
+            big = max(big & 0xFFFFu, big >> 16);
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+            const int qe = big >= 0x7F80u ? 0 : min(max((int)(big >> 7), 2) - 127, 126);   // (a subnormal row counts as 2^-125)
+            const float down = big >= 0x7F80u ? __uint_as_float(0x7FC00000u) : exp2_int(-qe);
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) {
+                qb[ks][0] = pack_f16(__uint_as_float(raw[ks].x << 16) * down, __uint_as_float(raw[ks].x & 0xFFFF0000u) * down);
+                qb[ks][1] = pack_f16(__uint_as_float(raw[ks].y << 16) * down, __uint_as_float(raw[ks].y & 0xFFFF0000u) * down);
+            }
+            const float f = exp2_int(qe) * p.scale_log2;
+            f0 = __shfl_sync(0xffffffffu, f, 8 * t);
+            f1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+        }
+        for (uint32_t j = ((uint32_t)warp + kWarps - at) % kWarps; j < n_blk; j += kWarps) {
+            if (!alive) break;
+            const uint32_t s = done % kStages;
+            alive = __all_sync(0xffffffffu, mbar_wait(full(s), (done / kStages) & 1u, abort_flag, p.status, kStatusTimeoutConsumer));
+            if (!alive) break;
+            const uint32_t blk = ring + s * kStageStride;
+            uint32_t scales;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(scales) : "r"(blk + kQ8ScaleOff));
+            const uint32_t ek = scales & 0xFFu, ev = scales >> 8;
+            const float nan = __uint_as_float(0x7FC00000u);
+            const float kf = ek == kQ8NoScale ? nan : exp2_int((int)ek - 127);
+            const float vx = ev == kQ8NoScale ? nan : (float)((int)ev - 127);
+            // S^T = K Q^T (two accumulators, so that the products do not wait for one another)
+            float sa[4] = {0.f, 0.f, 0.f, 0.f}, sb[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint4 x = lds128(blk + c * 512 + lane * 16);
+                uint32_t a0, a1, a2, a3;
+                decode4<kFmt>(x.x, a0, a2);
+                decode4<kFmt>(x.y, a1, a3);
+                mma_f16(sa, a0, a1, a2, a3, qb[2 * c][0], qb[2 * c][1]);
+                decode4<kFmt>(x.z, a0, a2);
+                decode4<kFmt>(x.w, a1, a3);
+                mma_f16(sb, a0, a1, a2, a3, qb[2 * c + 1][0], qb[2 * c + 1][1]);
+            }
+            const float k0 = f0 * kf, k1 = f1 * kf;
+            float s0 = (sa[0] + sb[0]) * k0, s1 = (sa[1] + sb[1]) * k1;  // token g, heads 2t and 2t + 1
+            float s2 = (sa[2] + sb[2]) * k0, s3 = (sa[3] + sb[3]) * k1;  // token g + 8
+            const uint32_t left = n_tok - j * kQ8Block;
+            if (left < (uint32_t)kQ8Block) {  // the cache ends inside the block
+                if ((uint32_t)g >= left) s0 = s1 = none;
+                if ((uint32_t)g + 8u >= left) s2 = s3 = none;
+            }
+            const float mx0 = fmaxf(s0, s2), mx1 = fmaxf(s1, s3);
+            const bool far = mx0 > m0 + kStep || mx1 > m1 + kStep || mx0 + vx > r0 + kStep || mx1 + vx > r1 + kStep;
+            if (__any_sync(0xffffffffu, far)) {
+                float c0 = mx0, c1 = mx1;
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    c0 = fmaxf(c0, __shfl_xor_sync(0xffffffffu, c0, d));
+                    c1 = fmaxf(c1, __shfl_xor_sync(0xffffffffu, c1, d));
+                }
+                // (a NaN takes no part in a maximum; it stays in the sums)
+                const float n0 = fmaxf(m0, c0), n1 = fmaxf(m1, c1), q0 = fmaxf(r0, c0 + vx), q1 = fmaxf(r1, c1 + vx);
+                l0 *= n0 == none ? 1.f : fast_exp2(m0 - n0);
+                l1 *= n1 == none ? 1.f : fast_exp2(m1 - n1);
+                const float a0 = q0 == none ? 1.f : fast_exp2(r0 - q0), a1 = q1 == none ? 1.f : fast_exp2(r1 - q1);
+                m0 = n0;
+                m1 = n1;
+                r0 = q0;
+                r1 = q1;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    o[i][0] *= a0;
+                    o[i][1] *= a1;
+                    o[i][2] *= a0;
+                    o[i][3] *= a1;
+                }
+            }
+            l0 += fast_exp2(s0 - m0) + fast_exp2(s2 - m0);
+            l1 += fast_exp2(s1 - m1) + fast_exp2(s3 - m1);
+            const float d0 = vx - r0, d1 = vx - r1;
+            const uint32_t b0 = transpose8x8(pack_f16(fast_exp2(s0 + d0), fast_exp2(s1 + d1)));
+            const uint32_t b1 = transpose8x8(pack_f16(fast_exp2(s2 + d0), fast_exp2(s3 + d1)));
+            // O^T += V^T w^T
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint4 x = lds128(blk + kQ8ValueOff + c * 512 + lane * 16);
+                uint32_t a0, a1, a2, a3;
+                decode4<kFmt>(x.x, a0, a2);
+                decode4<kFmt>(x.y, a1, a3);
+                if (kFmt == CART_Q8_E4M3 && left < (uint32_t)kQ8Block) {
+                    // codes behind the cache's end may be anything, NaN included: they count as zeros
+                    const uint32_t z0 = (2u * t < left ? 0xFFFFu : 0u) | (2u * t + 1u < left ? 0xFFFF0000u : 0u);
+                    const uint32_t z1 = (2u * t + 8u < left ? 0xFFFFu : 0u) | (2u * t + 9u < left ? 0xFFFF0000u : 0u);
+                    a0 &= z0;
+                    a1 &= z0;
+                    a2 &= z1;
+                    a3 &= z1;
+                }
+                mma_f16(o[2 * c], a0, a1, a2, a3, b0, b1);
+                decode4<kFmt>(x.z, a0, a2);
+                decode4<kFmt>(x.w, a1, a3);
+                if (kFmt == CART_Q8_E4M3 && left < (uint32_t)kQ8Block) {
+                    const uint32_t z0 = (2u * t < left ? 0xFFFFu : 0u) | (2u * t + 1u < left ? 0xFFFF0000u : 0u);
+                    const uint32_t z1 = (2u * t + 8u < left ? 0xFFFFu : 0u) | (2u * t + 9u < left ? 0xFFFF0000u : 0u);
+                    a0 &= z0;
+                    a1 &= z0;
+                    a2 &= z1;
+                    a3 &= z1;
+                }
+                mma_f16(o[2 * c + 1], a0, a1, a2, a3, b0, b1);
+            }
+            ++done;
+            __syncwarp();  // every lane has read the stage
+            issue_one();
+        }
+        at = (at + n_blk) % kWarps;
+        if (!(w.flags & CART_ITEM_END)) continue;
+
+        // ---- the piece's end: the warps' states meet in shared memory -------------------------------------------
+        float *ml = stat + (size_t)(piece & 1u) * kWarps * kMaxGroup * 3;
+        ++piece;
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, d);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, d);
+        }
+        if (g == 0) {
+            float *a = ml + ((size_t)warp * kMaxGroup + 2 * t) * 3;
+            a[0] = m0;
+            a[1] = l0;
+            a[2] = r0;
+            a[3] = m1;
+            a[4] = l1;
+            a[5] = r1;
+        }
+        __syncthreads();
+        {
+            float ra = none, rb = none;  // the largest reference R of the heads 2t, 2t + 1
+#pragma unroll
+            for (int x = 0; x < kWarps; ++x) {
+                ra = fmaxf(ra, ml[((size_t)x * kMaxGroup + 2 * t) * 3 + 2]);
+                rb = fmaxf(rb, ml[((size_t)x * kMaxGroup + 2 * t + 1) * 3 + 2]);
+            }
+            // (a warp that had no block of the piece holds zeros)
+            const float wa = r0 == ra ? 1.f : fast_exp2(r0 - ra), wb = r1 == rb ? 1.f : fast_exp2(r1 - rb);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                o[i][0] *= wa;
+                o[i][1] *= wb;
+                o[i][2] *= wa;
+                o[i][3] *= wb;
+            }
+            float *row = comb + (size_t)(warp % (kWarps / 2)) * kMaxGroup * kRowStride + (size_t)(2 * t) * kRowStride + g;
+            auto put = [&](bool add) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) {
+                        if (2 * t + hh >= G) continue;
+                        float *d = row + hh * kRowStride + 16 * i;
+                        d[0] = add ? d[0] + o[i][hh] : o[i][hh];
+                        d[8] = add ? d[8] + o[i][2 + hh] : o[i][2 + hh];
+                    }
+                }
+            };
+            if (warp >= kWarps / 2) put(false);
+            __syncthreads();
+            if (warp < kWarps / 2) put(true);
+            __syncthreads();
+        }
+        const bool direct = (w.flags & CART_ITEM_DIRECT) != 0u;
+        for (int x = threadIdx.x; x < G * 32; x += kStreamThreads) {
+            const int h = x >> 5, quad = x & 31;
+            float M = none, R = none, L = 0.f;
+#pragma unroll
+            for (int v = 0; v < kWarps; ++v) {
+                M = fmaxf(M, ml[((size_t)v * kMaxGroup + h) * 3]);
+                R = fmaxf(R, ml[((size_t)v * kMaxGroup + h) * 3 + 2]);
+            }
+#pragma unroll
+            for (int v = 0; v < kWarps; ++v) {
+                const float mv = ml[((size_t)v * kMaxGroup + h) * 3], lv = ml[((size_t)v * kMaxGroup + h) * 3 + 1];
+                L += mv == M ? lv : fast_exp2(mv - M) * lv;
+            }
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int v = 0; v < kWarps / 2; ++v) {
+                const float4 b = *reinterpret_cast<const float4 *>(comb + ((size_t)v * kMaxGroup + h) * kRowStride + 4 * quad);
+                a.x += b.x;
+                a.y += b.y;
+                a.z += b.z;
+                a.w += b.w;
+            }
+            const float lse2 = M + log2f(L);
+            // (R is -inf only where every value read was NaN, and the sums are)
+            const float f = R == none ? 1.f : exp2f(0.5f * (R - M));  // (in two factors: 2^(R - M) alone may leave fp32)
+            const float f2 = f / L;
+            a.x = a.x * f * f2;
+            a.y = a.y * f * f2;
+            a.z = a.z * f * f2;
+            a.w = a.w * f * f2;
+            if (direct) {
+                const size_t orow = (size_t)w.row_group * G + h;
+                uint2 packed;
+                packed.x = pack_bf16(a.x, a.y);
+                packed.y = pack_bf16(a.z, a.w);
+                *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + orow * kHeadDim + 4 * quad) = packed;
+                if (quad == 0 && p.lse) p.lse[orow] = lse2 * 0.6931471805599453f;
+            } else {
+                *(reinterpret_cast<float4 *>(p.part_o + ((size_t)w.slot * G + h) * kHeadDim) + quad) = a;
+                if (quad == 0) p.part_lse2[(size_t)w.slot * kMaxGroup + h] = lse2;
+            }
+        }
+        if (!direct && p.tickets != nullptr) {
+            // a split row group: the thread block whose piece arrives last merges all pieces; nobody waits
+            __threadfence();
+            __syncthreads();
+            const cart_merge_item mi = p.merges[w.merge];
+            if (threadIdx.x == 0)
+                *merge_flag = (*abort_flag == 0u && atomicAdd(&p.tickets[w.merge], 1u) + 1u == mi.slot_end - mi.slot_begin) ? 1u : 0u;
+            __syncthreads();
+            if (*merge_flag) {
+                __threadfence();
+                merge_row_group<1, 4>(mi, G, p.part_o, p.part_lse2, p.out, p.lse, (int)threadIdx.x, kStreamThreads);
+                if (threadIdx.x == 0) p.tickets[w.merge] = 0;  // ready for the next launch
+            }
+            __syncthreads();
+        }
+    }
+    if (!alive && lane == 0) {
+        // gave up: wait (bounded) for the copies still in flight before the thread block leaves
+        for (uint32_t u = done; u < issued; ++u) {
+            const uint64_t t0 = global_timer_ns();
+            while (!mbar_try_wait(full(u % kStages), (u / kStages) & 1u) && global_timer_ns() - t0 < kWaitLimitNs) {}
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t q8_prepare_kernels()
+{
+    cudaError_t e = cudaFuncSetAttribute(cart_q8_stream_kernel<CART_Q8_INT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStreamSmem);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(cart_q8_stream_kernel<CART_Q8_E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStreamSmem);
+}
+
+cudaError_t q8_launch_write(const Q8CopyParams &p, uint32_t n_tasks, cudaStream_t s)
+{
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = pdl_config((int)n_tasks, kCopyThreads, 0, s, &attr);
+    return p.format == CART_Q8_INT8 ? cudaLaunchKernelEx(&cfg, cart_q8_write_kernel<CART_Q8_INT8>, p)
+                                    : cudaLaunchKernelEx(&cfg, cart_q8_write_kernel<CART_Q8_E4M3>, p);
+}
+
+cudaError_t q8_launch_read(const Q8CopyParams &p, uint32_t n_tasks, cudaStream_t s)
+{
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = pdl_config((int)n_tasks, kCopyThreads, 0, s, &attr);
+    return p.format == CART_Q8_INT8 ? cudaLaunchKernelEx(&cfg, cart_q8_read_kernel<CART_Q8_INT8>, p)
+                                    : cudaLaunchKernelEx(&cfg, cart_q8_read_kernel<CART_Q8_E4M3>, p);
+}
+
+cudaError_t q8_launch_stream(const Q8StreamParams &p, int format, int grid, cudaStream_t s)
+{
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = pdl_config(grid, kStreamThreads, kStreamSmem, s, &attr);
+    return format == CART_Q8_INT8 ? cudaLaunchKernelEx(&cfg, cart_q8_stream_kernel<CART_Q8_INT8>, p)
+                                  : cudaLaunchKernelEx(&cfg, cart_q8_stream_kernel<CART_Q8_E4M3>, p);
+}
+
+}  // namespace cart

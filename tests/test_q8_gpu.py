@@ -1,0 +1,542 @@
+"""GPU parity of the caches in 8 bits against their float64 definitions (oracle/q8_oracle.py): storing and reading back
+bit for bit, attention within the error that the kernels' roundings may cause (derived in the oracle)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import q8_oracle as O
+from paper_2506_06266_b200 import binding as B, buildlib
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+FMT = {"int8": B.CART_Q8_INT8, "e4m3": B.CART_Q8_E4M3}
+
+
+class Pair:
+    """A context and, for every cache and layer, the definition's state."""
+
+    def __init__(self, hq, hkv, fmt="int8", layers=1, mb=64, rows=64, fill=0x7F, parts=8, **kw):
+        buildlib.build()
+        self.hq, self.hkv, self.fmt, self.L = hq, hkv, fmt, layers
+        cfg = B.make_config(layers, hq, hkv, rows, 8, max_parts=parts, **kw)
+        n = B.cart_scratch_bytes(cfg) + B.cart_q8_scratch_bytes(cfg) + (mb << 20)
+        self.arena = torch.full((n,), fill, dtype=torch.uint8, device=DEV)   # (0x7F: every code a NaN in e4m3)
+        cfg.arena, cfg.arena_bytes = self.arena.data_ptr(), n
+        self.cfg, self.ctx = cfg, B.cart_create(cfg)
+        self.scale = 128 ** -0.5
+        self.ref = {}
+
+    def open(self, parts=(), capacity=0):
+        c = B.cart_q8_open(self.ctx, FMT[self.fmt], parts, capacity)
+        self.ref[c] = [O.Cache(self.fmt, self.hkv, [self.ref[p][l] for p in parts]) for l in range(self.L)]
+        return c
+
+    def write(self, ids, ks, vs, first=None, layer=0):
+        """ks, vs: one bf16 tensor [n][hkv][128] per cache."""
+        k, v = torch.cat(ks).to(DEV), torch.cat(vs).to(DEV)
+        B.cart_q8_write(self.ctx, layer, ids, [x.shape[0] for x in ks], k, v, first=first)
+        torch.cuda.synchronize()
+        for i, c in enumerate(ids):
+            self.ref[c][layer].write(f64(ks[i]), f64(vs[i]), None if first is None else first[i])
+
+    def read(self, c, first=0, n=None, layer=0):
+        n = self.ref[c][layer].n - first if n is None else n
+        k = torch.full((n, self.hkv, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+        v = torch.full_like(k, 7.0)
+        B.cart_q8_read(self.ctx, layer, [c], [first], [n], k, v)
+        torch.cuda.synchronize()
+        return f64(k), f64(v)
+
+    def check_stored(self, c, layer=0):
+        k, v = self.read(c, layer=layer)
+        assert same(k, self.ref[c][layer].values(0)) and same(v, self.ref[c][layer].values(1))
+
+    def attend(self, ids, q, n_new=None, layer=0, extra=0):
+        rows = q.shape[0]
+        out = torch.full((rows + extra, self.hq, 128), 5.0, dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((rows + extra, self.hq), 5.0, dtype=torch.float32, device=DEV)
+        B.cart_q8_attention(self.ctx, layer, ids, q.to(DEV), out, lse, n_new=n_new)
+        B.cart_sync_status(self.ctx)
+        if extra:
+            assert torch.all(out[rows:] == 5.0) and torch.all(lse[rows:] == 5.0)
+        return out[:rows], lse[:rows]
+
+    def check(self, ids, q, out, lse, n_new=None, layer=0):
+        n_new = [1] * len(ids) if n_new is None else n_new
+        r = 0
+        for c, m in zip(ids, n_new):
+            if m == 0:
+                continue
+            o, l, to, tl = O.attention(self.ref[c][layer], f64(q[r:r + m]), self.scale)
+            do, dl = np.abs(f64(out[r:r + m]) - o), np.abs(f64(lse[r:r + m]) - l)
+            assert np.all(do <= to), "out: %g over its bound" % np.max(do / to)
+            assert np.all(dl <= tl), "lse: %g over its bound" % np.max(dl / tl)
+            r += m
+        assert r == q.shape[0]
+
+    def attend_and_check(self, ids, q, n_new=None, layer=0, extra=0):
+        out, lse = self.attend(ids, q, n_new, layer, extra)
+        self.check(ids, q, out, lse, n_new, layer)
+        return out, lse
+
+    def close(self):
+        B.cart_destroy(self.ctx)
+
+
+def f64(x):
+    return x.detach().to(torch.float64).cpu().numpy()
+
+
+def same(a, b):
+    return a.shape == b.shape and np.array_equal(np.isnan(a), np.isnan(b)) and np.array_equal(a[~np.isnan(a)], b[~np.isnan(b)])
+
+
+def rand(shape, seed, spread=0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g)
+    if spread:
+        x = x * 2.0 ** torch.randint(-spread, spread + 1, (shape[0],) + (1,) * (len(shape) - 1), generator=g)
+    return x.to(torch.bfloat16)
+
+
+@pytest.fixture
+def pair():
+    made = []
+
+    def make(*a, **kw):
+        made.append(Pair(*a, **kw))
+        return made[-1]
+    yield make
+    for p in made:
+        p.close()
+
+
+# ---- storing and reading back -------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 63, 64, 65, 129, 300])
+def test_written_at_once_reads_back_as_defined(pair, fmt, n):
+    p = pair(6, 3, fmt)
+    c = p.open()
+    p.write([c], [rand((n, 3, 128), n)], [rand((n, 3, 128), n + 1, 20)])
+    p.check_stored(c)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_ragged_batches_of_writes_with_rewinds_over_several_layers(pair, fmt):
+    p = pair(4, 2, fmt, layers=3)
+    rng = np.random.default_rng(5)
+    ids = [p.open(capacity=int(x)) for x in (0, 1, 64, 100, 300)]
+    for step in range(25):
+        layer = int(rng.integers(3))
+        who = [c for c in ids if rng.random() < 0.7] or ids[:1]
+        first = [int(rng.integers(max(0, p.ref[c][layer].n - 20), p.ref[c][layer].n + 1)) for c in who]
+        n = [int(rng.choice([0, 1, 1, 2, 7, 16, 40, 90])) for _ in who]
+        ks = [rand((m, 2, 128), 1000 + 7 * step + i, 6) for i, m in enumerate(n)]
+        vs = [rand((m, 2, 128), 5000 + 7 * step + i, 30) for i, m in enumerate(n)]
+        p.write(who, ks, vs, first, layer)
+    for c in ids:
+        for layer in range(3):
+            assert B.cart_q8_len(p.ctx, c, layer) == (p.ref[c][layer].n,) * 2
+            p.check_stored(c, layer)
+    # ranges that begin and end inside blocks, several caches in one call, one of them twice
+    first, n = [3, 17, 0, 3], [20, 1, 5, 9]
+    who = [ids[1], ids[2], ids[3], ids[1]]
+    k = torch.zeros((sum(n) + 2, 2, 128), dtype=torch.bfloat16, device=DEV)
+    v = torch.zeros_like(k)
+    B.cart_q8_read(p.ctx, 1, who, first, n, k[:-2], v[:-2])
+    want = [np.concatenate([p.ref[c][1].values(x)[f:f + m] for c, f, m in zip(who, first, n)]) for x in (0, 1)]
+    assert same(f64(k)[:-2], want[0]) and same(f64(v)[:-2], want[1])
+    assert torch.all(k[-2:] == 0) and torch.all(v[-2:] == 0)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_token_by_token_the_scale_grows_and_codes_are_rounded_once_more(pair, fmt):
+    p = pair(2, 2, fmt)
+    a, b = p.open(), p.open()
+    for t in range(70):
+        k, v = rand((1, 2, 128), t, 12), rand((1, 2, 128), 100 + t, 12)
+        p.write([a, b], [k, v], [v, k])
+    p.check_stored(a)
+    p.check_stored(b)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_extreme_values(pair, fmt):
+    p = pair(1, 1, fmt)
+    c = p.open()
+    x = torch.zeros((96, 1, 128))
+    x[0:16] = torch.linspace(-3.3e38, 3.3e38, 128)
+    x[16:32] = 1e-38 * torch.linspace(-1, 1, 128)
+    x[32:48, :, 0] = 448.0
+    x[33, :, 1:] = torch.linspace(0, 1.0, 127)
+    x[48:64, :, 0] = 127.0
+    x[48, :, 1:] = torch.arange(127) + 0.5
+    x[64:80, :, 0] = 255 * 2.0 ** -8                     # the mantissa of all ones: int8 needs the next exponent
+    x[80:96, :, 0] = 2.0 ** -133                         # the smallest bf16 there is
+    x = x.to(torch.bfloat16)
+    p.write([c], [x], [-x])
+    p.check_stored(c)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_a_block_with_a_nan_or_an_infinity_reads_as_nan_until_begun_anew(pair, fmt, bad):
+    p = pair(2, 2, fmt)
+    c = p.open()
+    k, v = rand((40, 2, 128), 1), rand((40, 2, 128), 2)
+    k[20, 1, 77] = bad
+    v[3, 0, 5] = bad
+    p.write([c], [k], [v])
+    p.check_stored(c)
+    assert np.isnan(p.read(c)[0][16:32, 1]).all() and np.isfinite(p.read(c)[0][:, 0]).all()
+    p.write([c], [rand((5, 2, 128), 3)], [rand((5, 2, 128), 4)], [30])   # into the marked block, and on
+    p.check_stored(c)
+    p.write([c], [rand((50, 2, 128), 5)], [rand((50, 2, 128), 6)], [0])  # all begun anew
+    p.check_stored(c)
+    assert np.isfinite(p.read(c)[0]).all()
+
+
+def test_strided_sources(pair):
+    p = pair(4, 2)
+    a, b = p.open(), p.open()
+    fused = rand((50, 4 + 2 + 2, 128), 9).to(DEV)        # [tokens][q | k | v heads][128]
+    k, v = fused[:, 4:6], fused[:, 6:8]
+    B.cart_q8_write(p.ctx, 0, [a], [50], k, v)
+    p.ref[a][0].write(f64(k), f64(v))
+    p.check_stored(a)
+    heads = rand((2, 50, 128), 10).to(DEV)               # head-major, as a Cartridge is
+    k = heads.transpose(0, 1)
+    B.cart_q8_write(p.ctx, 0, [b], [50], k, k)
+    p.ref[b][0].write(f64(k), f64(k))
+    p.check_stored(b)
+    one = rand((50, 1, 128), 11).to(DEV).expand(50, 2, 128)   # one head for all
+    B.cart_q8_write(p.ctx, 0, [b], [50], one, one, first=[7])
+    p.ref[b][0].write(f64(one), f64(one), 7)
+    p.check_stored(b)
+
+
+def test_a_quantised_cartridge_is_what_writing_its_tokens_gives(pair):
+    p = pair(4, 2, "e4m3", layers=2)
+    k, v = rand((2, 2, 100, 128), 1).to(DEV), rand((2, 2, 100, 128), 2).to(DEV)
+    cid = B.cart_register_cartridge(p.ctx, k, v, 100)
+    c = B.cart_q8_from_cartridge(p.ctx, cid, FMT["e4m3"])
+    B.cart_release_cartridge(p.ctx, cid)
+    p.ref[c] = [O.Cache("e4m3", 2) for _ in range(2)]
+    for layer in range(2):
+        p.ref[c][layer].write(f64(k[layer].transpose(0, 1)), f64(v[layer].transpose(0, 1)))
+        p.check_stored(c, layer)
+
+
+def test_many_caches_in_one_call(pair):
+    p = pair(1, 1, rows=300, mb=96)
+    ids = [p.open() for _ in range(290)]                 # more than one launch takes
+    n = [1 + i % 5 for i in range(290)]
+    p.write(ids, [rand((m, 1, 128), i) for i, m in enumerate(n)], [rand((m, 1, 128), 999 + i) for i, m in enumerate(n)])
+    for c in (ids[0], ids[119], ids[120], ids[239], ids[240], ids[289]):
+        p.check_stored(c)
+    p.attend_and_check(ids, rand((290, 1, 128), 3))
+
+
+# ---- attention ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (2, 1), (9, 3), (8, 2), (10, 2), (6, 1), (14, 2), (16, 2), (24, 8)])
+def test_decode_over_unequal_lengths(pair, fmt, hq, hkv):
+    p = pair(hq, hkv, fmt)
+    lens = [1, 2, 15, 16, 17, 64, 65, 200, 777]
+    ids = [p.open() for _ in lens]
+    p.write(ids, [rand((n, hkv, 128), n) for n in lens], [rand((n, hkv, 128), n + 1, 3) for n in lens])
+    p.attend_and_check(ids, 3 * rand((len(lens), hq, 128), 5), extra=3)
+    p.attend_and_check(ids[3:4], 3 * rand((1, hq, 128), 6))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_decode_long_caches_split_over_all_blocks(pair, fmt):
+    p = pair(8, 1, fmt, mb=96)
+    lens = [30000, 4097, 3]
+    ids = [p.open() for _ in lens]
+    p.write(ids, [rand((n, 1, 128), n) for n in lens], [rand((n, 1, 128), n + 1) for n in lens])
+    p.attend_and_check(ids, 2 * rand((3, 8, 128), 5))
+    p.attend_and_check([ids[0]], 20 * rand((1, 8, 128), 6))  # nearly one-hot
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_parts_in_order_shared_private_composed_and_alone(pair, fmt):
+    p = pair(6, 2, fmt)
+    z = [p.open() for _ in range(4)]
+    p.write(z, [rand((n, 2, 128), n) for n in (130, 5, 64, 300)], [rand((n, 2, 128), n + 9) for n in (130, 5, 64, 300)])
+    both = p.open([z[0], z[1]])                          # parts of its own and tokens: named as a part it stands for all three
+    p.write([both], [rand((20, 2, 128), 50)], [rand((20, 2, 128), 51)])
+    ids = [p.open(x) for x in ([z[0]], [z[1]], [z[0], z[2]], [both, z[3]], [z[2], z[2]], [z[3]], [])]
+    n = [3, 0, 70, 16, 1, 0, 40]
+    p.write(ids, [rand((m, 2, 128), 60 + m) for m in n], [rand((m, 2, 128), 70 + m) for m in n])
+    assert B.cart_q8_len(p.ctx, ids[3], 0) == (16, 130 + 5 + 20 + 300 + 16)
+    q = 2 * rand((7, 6, 128), 8)
+    p.attend_and_check(ids, q)
+    p.attend_and_check([ids[2], ids[2], ids[5]], q[:3])  # a cache may be asked twice
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("hq,hkv", [(3, 1), (16, 2)])
+def test_messages_are_causal(pair, fmt, hq, hkv):
+    p = pair(hq, hkv, fmt, rows=400)
+    z = p.open()
+    p.write([z], [rand((150, hkv, 128), 1)], [rand((150, hkv, 128), 2)])
+    ids = [p.open([z]), p.open(), p.open([z]), p.open([z]), p.open()]
+    n, new = [200, 33, 1, 64, 130], [130, 33, 1, 0, 17]
+    p.write(ids, [rand((m, hkv, 128), m) for m in n], [rand((m, hkv, 128), m + 1) for m in n])
+    p.attend_and_check(ids, 2 * rand((sum(new), hq, 128), 5), new, extra=2)
+    p.attend_and_check([ids[0]], 2 * rand((200, hq, 128), 6), [200])
+    p.attend_and_check([ids[0]], 2 * rand((2, hq, 128), 7), [2])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_what_lies_behind_a_cache_does_not_matter(pair, fmt):
+    # NaN and infinities in tokens dropped by a rewind, in other blocks and (after the block was begun anew) in none
+    p = pair(8, 2, fmt)
+    a, b = p.open(), p.open()
+    k, v = rand((90, 2, 128), 1), rand((90, 2, 128), 2)
+    k[40:], v[40:] = float("nan"), float("inf")
+    p.write([a, b], [k, k], [v, v])
+    p.write([a, b], [rand((8, 2, 128), 3), rand((0, 2, 128), 3)], [rand((8, 2, 128), 4), rand((0, 2, 128), 4)], [32, 32])
+    q = rand((2, 8, 128), 5)
+    out, lse = p.attend_and_check([a, b], q)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_a_nan_stays_with_the_rows_and_heads_that_see_it(pair, fmt):
+    p = pair(4, 2, fmt)
+    ids = [p.open() for _ in range(3)]
+    ks, vs = [rand((50, 2, 128), i) for i in range(3)], [rand((50, 2, 128), 9 + i) for i in range(3)]
+    ks[0][20, 0, 3] = float("nan")
+    vs[1][20, 1, 3] = float("inf")
+    p.write(ids, ks, vs)
+    q = rand((3, 4, 128), 5)
+    q[2, 1, 0] = float("inf")
+    out, lse = p.attend(ids, q)
+    bad = torch.isnan(out).all(-1).cpu()
+    assert bad.tolist() == [[True, True, False, False], [False, False, True, True], [False, True, False, False]]
+    assert torch.isfinite(out[~bad.to(DEV)]).all()
+    assert torch.isnan(lse).cpu().tolist() == [[True, True, False, False], [False] * 4, [False, True, False, False]]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("lo,hi", [(-100, 100), (-20, 20), (60, 110)])
+def test_scales_far_apart(pair, fmt, lo, hi):
+    p = pair(3, 1, fmt)
+    c = p.open()
+    n = 400
+    e = torch.linspace(lo, hi, n // 16)[torch.randperm(n // 16, generator=torch.Generator().manual_seed(1))].round()
+    v = (rand((n, 1, 128), 2).float() * 2.0 ** e.repeat_interleave(16)[:, None, None]).to(torch.bfloat16)
+    p.write([c], [rand((n, 1, 128), 1)], [v])
+    p.attend_and_check([c], 2 * rand((1, 3, 128), 3))
+    # keys and queries whose products are ordinary although neither is
+    d = p.open()
+    k = (rand((n, 1, 128), 4).float() * 2.0 ** 80).to(torch.bfloat16)
+    p.write([d], [k], [v])
+    p.attend_and_check([d], (rand((1, 3, 128), 5).float() * 2.0 ** -80).to(torch.bfloat16))
+
+
+def test_a_step_is_a_write_and_an_attention_over_many_steps_and_pages(pair):
+    for fmt in ("int8", "e4m3"):
+        p = pair(6, 2, fmt, layers=2)
+        z = p.open()
+        for layer in range(2):
+            p.write([z], [rand((100, 2, 128), layer)], [rand((100, 2, 128), 5 + layer)], layer=layer)
+        n = [1, 60, 64, 127, 0]
+        step, apart = [p.open([z]) for _ in n], [p.open([z]) for _ in n]
+        for layer in range(2):
+            for ids in (step, apart):
+                p.write(ids, [rand((m, 2, 128), m) for m in n], [rand((m, 2, 128), m + 3) for m in n], layer=layer)
+        launches = B.cart_launch_count(p.ctx)
+        for t in range(140):
+            for layer in range(2):
+                k, v, q = (rand((5, h, 128), 1000 * t + 10 * layer + i, 2).to(DEV) for i, h in enumerate((2, 2, 6)))
+                out, lse = torch.empty_like(q), torch.empty((5, 6), device=DEV)
+                B.cart_q8_decode_step(p.ctx, layer, step, k, v, q, out, lse)
+                for i, c in enumerate(step):
+                    p.ref[c][layer].write(f64(k[i:i + 1]), f64(v[i:i + 1]))
+                if t % 23 == 0 or t > 137:
+                    p.check(step, q, out, lse, layer=layer)
+                if t % 7 == 0 and layer == 0:            # a draft of three tokens is taken back, the step done again
+                    at = [p.ref[c][0].n - 1 for c in step]
+                    extra = rand((15, 2, 128), t)
+                    B.cart_q8_write(p.ctx, 0, step, [3] * 5, extra.to(DEV), extra.to(DEV))
+                    for i, c in enumerate(step):
+                        p.ref[c][0].write(f64(extra[3 * i:3 * i + 3]), f64(extra[3 * i:3 * i + 3]))
+                    B.cart_q8_decode_step(p.ctx, 0, step, k, v, q, out, lse, first=at)
+                    for i, c in enumerate(step):
+                        p.ref[c][0].write(f64(k[i:i + 1]), f64(v[i:i + 1]), at[i])
+                    p.check(step, q, out, lse)
+        B.cart_sync_status(p.ctx)
+        assert B.cart_launch_count(p.ctx) > launches
+        for c in step:
+            p.check_stored(c)
+            p.check_stored(c, 1)
+
+
+def test_results_repeat_bit_for_bit(pair):
+    p = pair(16, 2, mb=96)
+    ids = [p.open() for _ in range(3)]
+    p.write(ids, [rand((n, 2, 128), n) for n in (9000, 700, 1)], [rand((n, 2, 128), n + 1) for n in (9000, 700, 1)])
+    q = rand((3, 16, 128), 2)
+    first = p.attend(ids, q)
+    for _ in range(20):
+        again = p.attend(ids, q)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_beyond_four_gigabytes(pair):
+    p = pair(4, 1, "e4m3", mb=4700)
+    page = B.cart_q8_cache_bytes(p.cfg, 1)
+    p.open(capacity=64 * int((4500 << 20) // page))      # the pages of the first 4.5 GB, never written
+    c = p.open()
+    p.write([c], [rand((500, 1, 128), 1)], [rand((500, 1, 128), 2)])
+    p.check_stored(c)
+    p.attend_and_check([c], rand((1, 4, 128), 3))
+
+
+def test_another_stream_that_is_ordered_by_the_caller(pair):
+    p = pair(4, 2)
+    c = p.open()
+    k, v, q = rand((100, 2, 128), 1).to(DEV), rand((100, 2, 128), 2).to(DEV), rand((1, 4, 128), 3).to(DEV)
+    out, lse = torch.empty_like(q), torch.empty((1, 4), device=DEV)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    B.cart_q8_write(p.ctx, 0, [c], [100], k, v, stream=s1)
+    s2.wait_stream(s1)
+    B.cart_q8_attention(p.ctx, 0, [c], q, out, lse, stream=s2)
+    torch.cuda.synchronize()
+    p.ref[c][0].write(f64(k), f64(v))
+    p.check([c], q, out, lse)
+
+
+# ---- refusals ------------------------------------------------------------------------------------------------------------------
+
+def refused(status, f, *a, **kw):
+    with pytest.raises(B.CartError) as ei:
+        f(*a, **kw)
+    assert ei.value.status == status, ei.value
+
+
+def test_refusals_change_nothing(pair):
+    p = pair(4, 2, mb=4, rows=8, layers=1, parts=3)
+    x = rand((200, 2, 128), 1).to(DEV)
+    q = rand((9, 4, 128), 2).to(DEV)
+    out, lse = torch.empty_like(q), torch.empty((9, 4), device=DEV)
+    arg, handle, cap, oom, use, empty = (B.CART_ERR_INVALID_ARG, B.CART_ERR_BAD_HANDLE, B.CART_ERR_CAPACITY, B.CART_ERR_OOM,
+                                         B.CART_ERR_IN_USE, B.CART_ERR_EMPTY)
+    refused(handle, B.cart_q8_write, p.ctx, 0, [0], [1], x, x)           # nothing is open yet
+    refused(handle, B.cart_q8_attention, p.ctx, 0, [0], q, out)
+    refused(handle, B.cart_q8_read, p.ctx, 0, [0], [0], [0], x, x)
+    refused(handle, B.cart_q8_close, p.ctx, 0)
+    refused(handle, B.cart_q8_len, p.ctx, 0, 0)
+    refused(handle, B.cart_q8_from_cartridge, p.ctx, 0, B.CART_Q8_INT8)
+    z = p.open()
+    p.write([z], [x[:20].cpu()], [x[:20].cpu()])
+    c, d = p.open([z]), p.open()
+    other = B.cart_q8_open(p.ctx, B.CART_Q8_E4M3)
+    p.write([c], [x[:5].cpu()], [x[:5].cpu()])
+    refused(arg, B.cart_q8_open, p.ctx, 2)
+    refused(arg, B.cart_q8_open, p.ctx, B.CART_Q8_INT8, capacity=-1)
+    refused(arg, B.cart_q8_open, p.ctx, B.CART_Q8_E4M3, [z])             # another format
+    refused(handle, B.cart_q8_open, p.ctx, B.CART_Q8_INT8, [77])
+    refused(cap, B.cart_q8_open, p.ctx, B.CART_Q8_INT8, [z] * 4)
+    refused(oom, B.cart_q8_open, p.ctx, B.CART_Q8_INT8, [], 10 ** 7)
+    refused(use, B.cart_q8_close, p.ctx, z)
+    refused(use, B.cart_q8_write, p.ctx, 0, [z], [1], x, x)
+    refused(use, B.cart_q8_decode_step, p.ctx, 0, [z], x[:1], x[:1], q[:1], out[:1])
+    refused(handle, B.cart_q8_write, p.ctx, 1, [c], [1], x, x)           # no such layer
+    refused(handle, B.cart_q8_write, p.ctx, -1, [c], [1], x, x)
+    refused(arg, B.cart_q8_write, p.ctx, 0, [c, c], [1, 1], x, x)
+    refused(arg, B.cart_q8_write, p.ctx, 0, [c], [1], x, x, first=[6])   # a gap
+    refused(arg, B.cart_q8_write, p.ctx, 0, [c], [1], x, x, first=[-1])
+    refused(arg, B.cart_q8_write, p.ctx, 0, [c], [-1], x, x)
+    refused(arg, B.cart_q8_write, p.ctx, 0, [], [], x, x)
+    refused(arg, B.cart_q8_write, p.ctx, 0, [c, other], [1, 1], x, x)
+    refused(arg, B.cart_q8_write, p.ctx, 0, [c], [1], x.data_ptr() + 2, x.data_ptr(), strides=(256, 128))
+    refused(arg, B.cart_q8_write, p.ctx, 0, [c], [1], x.data_ptr(), x.data_ptr(), strides=(256, 4))
+    refused(arg, B.cart_q8_write, p.ctx, 0, [c], [1], x.data_ptr(), x.data_ptr(), strides=(-256, 128))
+    refused(arg, B.cart_q8_write, p.ctx, 0, [c], [1], None, None)
+    refused(oom, B.cart_q8_write, p.ctx, 0, [d, c], [1, 10 ** 6], x, x)
+    refused(arg, B.cart_q8_read, p.ctx, 0, [c], [0], [6], x, x)
+    refused(arg, B.cart_q8_read, p.ctx, 0, [c], [-1], [1], x, x)
+    refused(arg, B.cart_q8_read, p.ctx, 0, [c], [0], [1], None, x)
+    refused(arg, B.cart_q8_attention, p.ctx, 0, [], q, out)
+    refused(arg, B.cart_q8_attention, p.ctx, 0, [c], q, out, n_new=[6])
+    refused(arg, B.cart_q8_attention, p.ctx, 0, [c], q, out, n_new=[-1])
+    refused(arg, B.cart_q8_attention, p.ctx, 0, [c, other], q, out)
+    refused(arg, B.cart_q8_attention, p.ctx, 0, [c], None, out)
+    refused(arg, B.cart_q8_attention, p.ctx, 0, [c], q, out.data_ptr() + 2)
+    refused(empty, B.cart_q8_attention, p.ctx, 0, [c, d], q, out)
+    refused(cap, B.cart_q8_attention, p.ctx, 0, [c] * 9, q, out)         # nine rows, eight are the most
+    refused(arg, B.cart_q8_decode_step, p.ctx, 0, [c, c], x[:2], x[:2], q[:2], out[:2])
+    refused(handle, B.cart_q8_len, p.ctx, c, 1)
+    with pytest.raises(ValueError):
+        B.cart_q8_attention(p.ctx, 0, [c], q.half(), out)
+    with pytest.raises(ValueError):
+        B.cart_q8_attention(p.ctx, 0, [c], q.transpose(0, 1), out)
+    with pytest.raises(ValueError):
+        B.cart_q8_write(p.ctx, 0, [c], [1, 2], x, x)
+    with pytest.raises(ValueError):
+        B.cart_q8_write(p.ctx, 0, [c], [1], x.float(), x.float())
+    # captured streams
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s = torch.cuda.current_stream()
+        refused(arg, B.cart_q8_write, p.ctx, 0, [c], [1], x, x, stream=s)
+        refused(arg, B.cart_q8_attention, p.ctx, 0, [c], q, out, stream=s)
+        refused(arg, B.cart_q8_decode_step, p.ctx, 0, [c], x[:1], x[:1], q[:1], out[:1], stream=s)
+        refused(arg, B.cart_q8_read, p.ctx, 0, [c], [0], [1], x, x, stream=s)
+    # and all is as before
+    assert B.cart_q8_len(p.ctx, c, 0) == (5, 25) and B.cart_q8_len(p.ctx, d, 0) == (0, 0)
+    p.check_stored(c)
+    p.attend_and_check([c], q[:1].cpu())
+    B.cart_q8_write(p.ctx, 0, [c], [0], None, None, first=[2])           # a rewind alone
+    assert B.cart_q8_len(p.ctx, c, 0) == (2, 22)
+    B.cart_q8_attention(p.ctx, 0, [c], None, None, n_new=[0])            # nobody asks
+    B.cart_q8_close(p.ctx, c)
+    B.cart_q8_close(p.ctx, z)
+    refused(handle, B.cart_q8_close, p.ctx, z)
+
+
+# ---- a run of them together ------------------------------------------------------------------------------------------------------
+
+def test_serving_with_an_8_bit_cartridge(pair):
+    """A trained Cartridge is registered in bf16, quantised and shared by users, whose messages and decode steps go on top; the
+    same in bf16 gives what quantisation leaves of it."""
+    p = pair(8, 2, "int8", layers=2, rows=128)
+    kz, vz = rand((2, 2, 200, 128), 1).to(DEV), rand((2, 2, 200, 128), 2).to(DEV)
+    cid = B.cart_register_cartridge(p.ctx, kz, vz, 200)
+    z = B.cart_q8_from_cartridge(p.ctx, cid, B.CART_Q8_INT8)
+    p.ref[z] = [O.Cache("int8", 2) for _ in range(2)]
+    users, plain = [p.open([z]) for _ in range(3)], [B.cart_request_open(p.ctx, cid, 128) for _ in range(3)]
+    msg = [9, 30, 1]
+    for layer in range(2):
+        p.ref[z][layer].write(f64(kz[layer].transpose(0, 1)), f64(vz[layer].transpose(0, 1)))
+        ks, vs = [rand((m, 2, 128), 10 + m) for m in msg], [rand((m, 2, 128), 20 + m) for m in msg]
+        p.write(users, ks, vs, layer=layer)
+        q = rand((sum(msg), 8, 128), 30 + layer)
+        out, lse = p.attend_and_check(users, q, msg, layer)
+        r = 0
+        for u, k, v in zip(plain, ks, vs):
+            m = k.shape[0]
+            B.cart_extend_kv(p.ctx, layer, u, k.to(DEV), v.to(DEV), m)
+            o = torch.empty((m, 8, 128), dtype=torch.bfloat16, device=DEV)
+            B.cart_prefill_attention(p.ctx, layer, u, q[r:r + m].to(DEV).contiguous(), m, o)
+            assert float((o.float() - out[r:r + m].float()).norm() / o.float().norm()) < 0.05
+            r += m
+    for t in range(5):
+        for layer in range(2):
+            k, v, q = (rand((3, h, 128), 100 * t + layer + i).to(DEV) for i, h in enumerate((2, 2, 8)))
+            out, lse = torch.empty_like(q), torch.empty((3, 8), device=DEV)
+            B.cart_q8_decode_step(p.ctx, layer, users, k, v, q, out, lse)
+            for i, c in enumerate(users):
+                p.ref[c][layer].write(f64(k[i:i + 1]), f64(v[i:i + 1]))
+            p.check(users, q, out, lse, layer=layer)
+            o = torch.empty_like(out)
+            B.cart_decode_step(p.ctx, layer, plain, k, v, q, o)
+            assert float((o.float() - out.float()).norm() / o.float().norm()) < 0.05
+    B.cart_sync_status(p.ctx)

@@ -1,0 +1,125 @@
+"""The float64 definitions of the caches in 8 bits against closed forms and brute force (no GPU), and what the library
+answers without a device."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import q8_oracle as O
+from paper_2506_06266_b200 import binding, buildlib
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    buildlib.build()
+    return binding.load_library()
+
+
+def all_e4m3():
+    """Every finite e4m3 number, from the format's definition."""
+    vals = []
+    for s in (1.0, -1.0):
+        for e in range(16):
+            for m in range(8):
+                if e == 15 and m == 7:
+                    continue
+                vals.append(s * (m / 8 * 2.0 ** -6 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7)))
+    return np.unique(np.array(vals))
+
+
+def test_grid_of_e4m3_is_the_nearest_of_all_codes():
+    codes = all_e4m3()
+    assert codes.max() == 448 and len(codes) == 253
+    y = np.random.default_rng(0).standard_normal(4000) * 10.0 ** np.random.default_rng(1).uniform(-4, 2, 4000)
+    y = y[np.abs(y) <= 448]
+    got = O.to_grid(y, "e4m3")
+    assert np.all(np.isin(got, codes))
+    assert np.allclose(np.abs(got - y), np.min(np.abs(codes[None] - y[:, None]), axis=1), rtol=0, atol=1e-15)
+    # ties go to the even mantissa: halfway between 1 and 1.125, and between 1.125 and 1.25
+    assert O.to_grid(np.array([1.0625, 1.1875, 2.0 ** -10, 3 * 2.0 ** -10]), "e4m3").tolist() == [1.0, 1.25, 0.0, 2.0 ** -8]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_exponent_is_the_smallest_that_fits(fmt):
+    for x in [1.0, O.TOP[fmt], np.nextafter(O.TOP[fmt], 1e9), 0.3, 2.0 ** 60, 3.3e38, 2.0 ** -100]:
+        e = O.exponent(np.array([x, -x / 2]), fmt)
+        assert x <= O.TOP[fmt] * 2.0 ** e and (e == O.E_MIN or x > O.TOP[fmt] * 2.0 ** (e - 1))
+    assert O.exponent(np.zeros(3), fmt) == O.E_MIN and O.exponent(np.array([1e-44]), fmt) == O.E_MIN
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_written_at_once_or_token_by_token_stays_within_the_stated_error(fmt):
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((50, 2, 128)) * 2.0 ** rng.integers(-8, 9, (50, 1, 1))   # every block's scale grows several times
+    once, each = O.Cache(fmt, 2), O.Cache(fmt, 2)
+    once.write(x, x)
+    for t in range(50):
+        each.write(x[t:t + 1], x[t:t + 1])
+    for c, grown in ((once, False), (each, True)):
+        got, step = c.values(0), c.scales(0)[:, :, None]
+        err = np.abs(got - x)
+        if fmt == "int8":
+            assert np.all(err <= (1.0 if grown else 0.5) * step)
+        else:
+            # each rounding: 2^-4 of the value, or half the smallest step; a raise re-rounds only what falls below 2^-6 of a step
+            assert np.all(err <= 2.0 ** -4 * np.abs(x) + (2 if grown else 1) * 2.0 ** -10 * step)
+    assert np.array_equal(once.scales(0)[-2:], each.scales(0)[-2:])
+
+
+def test_a_block_without_a_scale_recovers_only_when_begun_anew():
+    c = O.Cache("int8", 1)
+    x = np.ones((20, 1, 128))
+    c.write(x, x)
+    bad = np.ones((1, 1, 128))
+    bad[0, 0, 5] = np.inf
+    c.write(bad, np.ones((1, 1, 128)), first=18)
+    assert np.all(np.isnan(c.values(0)[16:])) and np.all(c.values(0)[:16] == 1) and np.all(c.values(1) == 1)
+    c.write(np.ones((1, 1, 128)), np.ones((1, 1, 128)), first=17)
+    assert c.n == 18 and np.all(np.isnan(c.values(0)[16:]))
+    c.write(np.ones((3, 1, 128)), np.ones((3, 1, 128)), first=16)
+    assert np.all(c.values(0) == 1)
+
+
+def test_attention_closed_forms():
+    one = O.Cache("int8", 1)
+    one.write(np.full((1, 1, 128), 0.5), np.full((1, 1, 128), 3.0))
+    out, lse, _, _ = O.attention(one, np.ones((1, 2, 128)), 0.1)
+    assert np.all(out == 3.0) and np.allclose(lse, 0.1 * 64)
+    # equal keys: the mean of the values; a part in front counts as tokens in front
+    back = O.Cache("e4m3", 1)
+    back.write(np.zeros((3, 1, 128)), np.arange(1.0, 4.0)[:, None, None] * np.ones((1, 1, 128)))
+    c = O.Cache("e4m3", 1, [back])
+    c.write(np.zeros((2, 1, 128)), np.array([6.0, 8.0])[:, None, None] * np.ones((1, 1, 128)))
+    out, lse, _, _ = O.attention(c, np.ones((2, 1, 128)), 1.0)
+    assert np.allclose(out[0], 12 / 4) and np.allclose(out[1], 20 / 5) and np.allclose(lse[:, 0], np.log([4, 5]))
+
+
+def test_sizes_need_no_device():
+    cfg = binding.make_config(28, 24, 8, 64, 64)
+    assert binding.cart_q8_scratch_bytes(cfg) % 256 == 0
+    page = binding.cart_q8_cache_bytes(cfg, 1)
+    assert binding.cart_q8_cache_bytes(cfg, 0) == 0 and binding.cart_q8_cache_bytes(cfg, 64) == page
+    assert binding.cart_q8_cache_bytes(cfg, 65) == 2 * page
+    # half the bytes of bf16, and 16 more for every 16 tokens
+    assert 28 * 8 * 64 * 256 < page < 28 * 8 * 64 * 256 * 1.01
+    for f in (binding.cart_q8_scratch_bytes, lambda c: binding.cart_q8_cache_bytes(c, 5)):
+        with pytest.raises(binding.CartError) as ei:
+            f(binding.make_config(28, 24, 7, 64, 64))
+        assert ei.value.status == binding.CART_ERR_SHAPE
+    with pytest.raises(binding.CartError) as ei:
+        binding.cart_q8_cache_bytes(cfg, -1)
+    assert ei.value.status == binding.CART_ERR_INVALID_ARG
+
+
+def test_every_call_refuses_a_missing_context(lib):
+    n = ctypes.c_int32(0)
+    one = (ctypes.c_int32 * 1)(0)
+    bad = binding.CART_ERR_INVALID_ARG
+    assert lib.cart_q8_open(None, 0, None, 0, 0, ctypes.byref(n)) == bad
+    assert lib.cart_q8_close(None, 0) == bad
+    assert lib.cart_q8_from_cartridge(None, 0, 0, None, ctypes.byref(n)) == bad
+    assert lib.cart_q8_write(None, 0, one, 1, None, one, 16, 16, 8, 8, None) == bad
+    assert lib.cart_q8_read(None, 0, one, 1, one, one, 16, 16, None) == bad
+    assert lib.cart_q8_attention(None, 0, one, 1, None, 16, 16, None, None) == bad
+    assert lib.cart_q8_decode_step(None, 0, one, 1, None, 16, 16, 16, 16, None, None) == bad
+    assert lib.cart_q8_len(None, 0, 0, None, None) == bad
