@@ -193,10 +193,10 @@ def prepare(case, seed):
         ctx = binding.cart_create(cfg)
         fmt = {"int8": binding.CART_Q8_INT8, "e4m3": binding.CART_Q8_E4M3}[case["fmt"]]
         here = torch.cuda.current_stream()
-        ids = [binding.cart_q8_open(ctx, fmt) for _ in range(n_parts)]
-        ids += [binding.cart_q8_open(ctx, fmt, [ids[j] for j in parts[i]], own_len[i]) for i in range(n)]
-        held = part_len + (own_len if op == "attend" else first)
-        for i, t in enumerate(held):
+        ids = []
+        for i, t in enumerate(part_len + (own_len if op == "attend" else first)):   # a Cartridge is written before it is a part
+            mine = [] if i < n_parts else [ids[j] for j in parts[i - n_parts]]
+            ids.append(binding.cart_q8_open(ctx, fmt, mine, lens[i]))
             if t:
                 binding.cart_q8_write(ctx, 0, [ids[i]], [t], k[at[i]:at[i] + t], v[at[i]:at[i] + t], stream=here)
         state |= {"b": binding, "ctx": _Context(binding, ctx, arena), "ids": binding.ReqList(ids[n_parts:])}
