@@ -17,12 +17,10 @@ constexpr uint64_t kQ8Align = 256;
 
 uint64_t up(uint64_t x) { return (x + kQ8Align - 1) / kQ8Align * kQ8Align; }
 
-// One slot: [cta_begin][merges][items] [unit_cta_begin][readers][reader_slot][reader_merge][units] [pages]; then, behind
-// the slots, the split partials, and in front of them the arrival tickets.  A function of the configuration alone.
+// Arrival tickets, then the slots (a plan's tables or a page list, packed back to back), then the split partials.  A
+// function of the configuration alone.
 struct Q8Layout {
-    uint64_t tickets_bytes;
-    uint64_t merges_off, items_off, unit_cta_off, readers_off, reader_slot_off, reader_merge_off, units_off, pages_off;
-    uint64_t slot_bytes, part_o_off, part_lse_off, total;
+    uint64_t tickets_bytes, slot_bytes, part_o_off, part_lse_off, total;
     int items_cap, merges_cap, slots_cap, units_cap, readers_cap, pages_cap;
 };
 
@@ -40,15 +38,10 @@ Q8Layout q8_layout(const cart_config &c)
     s.units_cap = s.readers_cap * c.n_kv_heads + kQ8MaxCta;
     s.pages_cap = 256 * c.max_requests + 65536;  // 16 k tokens a request on average, and 4 M tokens besides
     s.tickets_bytes = up((uint64_t)s.merges_cap * 4);
-    s.merges_off = up((uint64_t)(kQ8MaxCta + 1) * 4);
-    s.items_off = s.merges_off + up((uint64_t)s.merges_cap * sizeof(cart_merge_item));
-    s.unit_cta_off = s.items_off + up((uint64_t)s.items_cap * sizeof(cart_work_item));
-    s.readers_off = s.unit_cta_off + up((uint64_t)(kQ8MaxCta + 1) * 4);
-    s.reader_slot_off = s.readers_off + up((uint64_t)s.readers_cap * 4);
-    s.reader_merge_off = s.reader_slot_off + up((uint64_t)s.readers_cap * c.n_kv_heads * 4);
-    s.units_off = s.reader_merge_off + up((uint64_t)s.readers_cap * c.n_kv_heads * 4);
-    s.pages_off = s.units_off + up((uint64_t)s.units_cap * sizeof(cart_shared_unit));
-    s.slot_bytes = s.pages_off + up((uint64_t)s.pages_cap * 4);
+    s.slot_bytes = 2 * up((uint64_t)(kQ8MaxCta + 1) * 4) + up((uint64_t)(kQ8MaxCta + 1) * 4) +
+                   up((uint64_t)s.merges_cap * sizeof(cart_merge_item)) + up((uint64_t)s.items_cap * sizeof(cart_work_item)) +
+                   up((uint64_t)s.readers_cap * 4) + up((uint64_t)s.readers_cap * c.n_kv_heads * 4) +
+                   up((uint64_t)s.units_cap * sizeof(cart_shared_unit)) + up((uint64_t)s.pages_cap * 4) + 16 * kQ8Align;
     s.part_o_off = s.tickets_bytes + (uint64_t)kQ8Slots * s.slot_bytes;
     s.part_lse_off = s.part_o_off + up((uint64_t)s.slots_cap * group * kHeadDim * 4);
     s.total = s.part_lse_off + up((uint64_t)s.slots_cap * kMaxGroup * 4);
@@ -89,7 +82,16 @@ struct Slot {
     std::vector<int32_t> key;     // what it was built for, besides lens
     std::vector<int32_t> lens;    // kDecode: own lengths when it was built
     std::vector<uint32_t> bases;  // per cache of the call: index of its page 0 in the page list
-    int32_t n_items = 0, n_merges = 0, n_cta_used = 0, n_units = 0, n_unit_cta_used = 0;
+    // a plan's tables (offsets into the slot); the page list comes first
+    uint64_t cta_off = 0, items_off = 0, merges_off = 0;
+    int32_t n_items = 0, n_merges = 0, n_cta_used = 0;
+    struct Tiles { uint64_t cta_off = 0, units_off = 0, readers_off = 0, slots_off = 0; int32_t n_cta = 0; } tiles[2];  // shared parts; messages
+};
+
+// Work for the tcgen05 kernel, as its tables want it.
+struct TileWork {
+    std::vector<cart_shared_unit> units;
+    std::vector<uint32_t> cta, readers, slots;  // units before block c; query row per reader; first slot per (reader, KV head)
 };
 
 }  // namespace
@@ -101,8 +103,12 @@ struct Q8State {
     std::vector<Cache> caches;
     Slot slots[kQ8Slots];
     uint64_t epoch = 1, stamp = 0, list_stamp = 0, clock = 0;
-    std::vector<int32_t> key_tmp, len_tmp, seg_begin_tmp, first_tmp, cnt_tmp;
+    std::vector<int32_t> key_tmp, len_tmp, seg_begin_tmp;
     std::vector<cart_plan_seg> seg_tmp;
+    std::vector<cart_work_item> item_tmp;
+    std::vector<cart_merge_item> merge_tmp;
+    std::vector<uint32_t> cta_tmp, row_tmp;
+    TileWork work_tmp[2];
 };
 
 void q8_release(Q8State *st)
@@ -172,6 +178,7 @@ cart_status make_state(cart_ctx *ctx)
     }
     st->base = static_cast<uint8_t *>(v.cfg->arena) + st->start * kRowBytes;
     cudaError_t e = q8_prepare_kernels();
+    if (e == cudaSuccess) e = q8_prepare_tile_kernels();
     if (e == cudaSuccess) e = cudaMemset(st->base, 0, st->lay.tickets_bytes);
     for (int i = 0; i < kQ8Slots && e == cudaSuccess; ++i) {
         Slot &s = st->slots[i];
@@ -277,12 +284,12 @@ cart_status list_slot(cart_ctx *ctx, const cart_q8 *ids, int32_t n, cudaStream_t
     sl->bases.clear();
     for (int32_t i = 0; i < n; ++i) {
         Cache &c = st->caches[(size_t)ids[i]];
-        if (!list_pages(st, c, reinterpret_cast<uint32_t *>(sl->host + st->lay.pages_off), &n_listed))
+        if (!list_pages(st, c, reinterpret_cast<uint32_t *>(sl->host), &n_listed))
             return ctx_fail(ctx, CART_ERR_CAPACITY, "q8: the batch names more than %d pages", st->lay.pages_cap);
         sl->bases.push_back(c.list_base);
     }
     if (n_listed > 0)
-        Q8_CUDA(ctx, cudaMemcpyAsync(sl->dev + st->lay.pages_off, sl->host + st->lay.pages_off, (size_t)n_listed * 4,
+        Q8_CUDA(ctx, cudaMemcpyAsync(sl->dev, sl->host, (size_t)n_listed * 4,
                                      cudaMemcpyHostToDevice, s));
     use_slot(st, sl, s);  // (the copy reads the host buffer)
     sl->key.assign(ids, ids + n);
@@ -301,7 +308,7 @@ cart_status launch_copy(cart_ctx *ctx, bool write, const Slot *sl, int32_t layer
     static_assert(sizeof(Q8CopyParams) <= 4096, "the parameters must fit the kernel parameter space");
     Q8CopyParams p;
     p.arena = static_cast<uint8_t *>(cv.cfg->arena);
-    p.pages = reinterpret_cast<const uint32_t *>(sl->dev + st->lay.pages_off);
+    p.pages = reinterpret_cast<const uint32_t *>(sl->dev);
     p.k = k;
     p.v = v;
     p.token_stride = tok_stride;
@@ -364,6 +371,180 @@ cart_status prepare_write(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int3
     return CART_OK;
 }
 
+// A cache whose last n_rows tokens ask, query rows row0 .. row0 + n_rows - 1.
+struct Message {
+    const Cache *c;
+    uint32_t row0;
+    int32_t n_rows, len;
+};
+
+// Messages of at least this many rows run as chains of tiles on the tcgen05 kernel, shorter ones row by row on the
+// stream kernel: a tile of 128 tokens takes the one as long as the other about three rows.
+constexpr int kChainRows = 4;
+// What a chain's piece costs a block beside its tiles (its rows fetched, its result written), in tile times.
+constexpr uint32_t kPieceTiles = 3;
+
+// Messages as chains of units (cart_plan.h): rows of messages that stand behind the same parts are packed into M-tiles
+// of 128 / G; a chain is an M-tile times a KV head, over the parts' tiles, then message by message the tiles of the
+// tokens that its rows see, masked causally.  All chains laid end to end are cut into equal shares, one per block.  A
+// chain in one piece writes its rows itself; the pieces of a cut one leave partials for the merge kernel.  Returns the
+// number of blocks.
+int32_t plan_messages(const Q8State *st, const CtxView &cv, int32_t layer, std::vector<Message> &messages, int n_cta, int32_t slots_cap,
+                      int32_t *n_slots, std::vector<cart_merge_item> *merges, TileWork *w)
+{
+    const uint32_t Hkv = (uint32_t)cv.cfg->n_kv_heads, tpt = 128u / (uint32_t)cv.group;
+    std::stable_sort(messages.begin(), messages.end(), [](const Message &a, const Message &b) { return a.c->parts < b.c->parts; });
+    // the runs of every M-tile (the same for all KV heads): units without their KV head, and how many tiles they have
+    struct Tile { uint32_t reader_begin, n_readers, first_run, n_runs, n_tiles; };
+    std::vector<Tile> m_tiles;
+    std::vector<cart_shared_unit> runs;
+    constexpr uint32_t T = (uint32_t)kShareTileTokens;
+    for (size_t a = 0; a < messages.size();) {
+        size_t b = a;
+        uint32_t rows = 0;
+        while (b < messages.size() && messages[b].c->parts == messages[a].c->parts) rows += (uint32_t)messages[b++].n_rows;
+        const uint32_t reader0 = (uint32_t)w->readers.size();
+        for (size_t x = a; x < b; ++x)
+            for (int32_t r = 0; r < messages[x].n_rows; ++r) w->readers.push_back(messages[x].row0 + (uint32_t)r);
+        for (uint32_t r0 = 0; r0 < rows; r0 += tpt) {
+            Tile t{reader0 + r0, std::min(tpt, rows - r0), (uint32_t)runs.size(), 0u, 0u};
+            auto add = [&](uint32_t list_base, uint32_t n_tok, int32_t lim_base, uint32_t tr_lo, uint32_t tr_hi, uint32_t flags) {
+                cart_shared_unit u{};
+                u.k_row = list_base;
+                u.layer_stride = Hkv;
+                u.n_tiles = (n_tok + T - 1) / T;
+                u.reader_begin = t.reader_begin;
+                u.n_readers = t.n_readers;
+                u.flags = (uint16_t)(CART_UNIT_PAGED | flags);
+                u.lim_base = lim_base;
+                u.lim_cap = (int32_t)n_tok - 1;
+                u.tr_hi = tr_lo << 16 | tr_hi;
+                runs.push_back(u);
+                ++t.n_runs;
+                t.n_tiles += u.n_tiles;
+            };
+            for (int32_t q : messages[a].c->parts) {
+                const Cache &c = st->caches[(size_t)q];
+                const int32_t n = c.len[(size_t)layer];
+                // (every row sees all of it; a ragged end is masked as the end of the run)
+                if (n > 0) add(c.list_base, (uint32_t)n, n - 1, 0u, 0xFFFFu, (uint32_t)n % T ? CART_UNIT_MASKED : 0u);
+            }
+            uint32_t at = 0;   // first row of message x among the pack's
+            for (size_t x = a; x < b; at += (uint32_t)messages[x].n_rows, ++x) {
+                const Message &m = messages[x];
+                const uint32_t lo = std::max(at, r0), hi = std::min(at + (uint32_t)m.n_rows, r0 + t.n_readers);
+                if (lo >= hi) continue;
+                const int32_t key0 = m.len - m.n_rows;   // row r of the message sees its tokens 0 .. key0 + r
+                add(m.c->list_base, (uint32_t)(key0 + (int32_t)(hi - 1 - at) + 1), key0 + (int32_t)r0 - (int32_t)at, lo - r0, hi - r0,
+                    CART_UNIT_MASKED | CART_UNIT_SUFFIX);
+            }
+            m_tiles.push_back(t);
+        }
+        a = b;
+    }
+    uint64_t W = 0;
+    for (const Tile &t : m_tiles) W += (uint64_t)t.n_tiles * Hkv;
+    const uint64_t n_chains = (uint64_t)m_tiles.size() * Hkv;
+    w->slots.assign(w->readers.size() * Hkv, 0u);
+    struct Piece { uint32_t tile, head, t0, t1; };
+    std::vector<Piece> pieces;
+    std::vector<uint32_t> first;   // pieces before block c
+    uint64_t C = std::min<uint64_t>((uint64_t)n_cta, std::max<uint64_t>(1, W / 2));
+    for (;; C = (C + 1) / 2) {
+        pieces.clear();
+        first.assign(1, 0u);
+        uint64_t tiles_left = W, chains_left = n_chains, budget = 0, acc = 0, c = 0;
+        auto open = [&](bool mid) {   // an equal share of the weight that is left, counting a cut for every block still to come
+            const uint64_t blocks = C - c;
+            budget = (tiles_left + kPieceTiles * (chains_left + (mid ? 1 : 0) + (blocks - 1)) + blocks - 1) / blocks;
+            acc = 0;
+        };
+        open(false);
+        int64_t need = 0;
+        for (size_t i = 0; i < m_tiles.size(); ++i)
+            for (uint32_t h = 0; h < Hkv; ++h) {
+                const uint32_t n = m_tiles[i].n_tiles;
+                uint32_t done = 0, cut = 0;
+                while (done < n) {
+                    uint32_t take = n - done;
+                    if (c + 1 < C) {
+                        const uint64_t room = budget > acc + kPieceTiles ? budget - acc - kPieceTiles : 0;
+                        if (room < 2 && acc > 0) {   // too little left for a piece
+                            first.push_back((uint32_t)pieces.size());
+                            ++c;
+                            open(done > 0);
+                            continue;
+                        }
+                        // (no piece of less than two tiles is left behind)
+                        if (take > room) take = (uint32_t)std::max<uint64_t>(room, 2);
+                        if (n - done - std::min(take, n - done) < 2) take = n - done;
+                    }
+                    pieces.push_back(Piece{(uint32_t)i, h, done, done + take});
+                    acc += take + kPieceTiles;
+                    tiles_left -= take;
+                    if (done == 0) --chains_left;
+                    done += take;
+                    ++cut;
+                }
+                if (cut > 1) need += (int64_t)cut * m_tiles[i].n_readers;
+            }
+        first.push_back((uint32_t)pieces.size());
+        if (need + *n_slots <= slots_cap || C == 1) break;
+    }
+    // units, slots and merge items, piece by piece
+    w->cta.assign(1, 0u);
+    size_t block_end = 1;
+    uint32_t chunk = 0;
+    for (size_t x = 0; x < pieces.size(); ++x) {
+        while (x == first[block_end]) {
+            w->cta.push_back((uint32_t)w->units.size());
+            ++block_end;
+        }
+        const Piece &pc = pieces[x];
+        const Tile &t = m_tiles[pc.tile];
+        const bool whole = pc.t0 == 0 && pc.t1 == t.n_tiles;
+        chunk = pc.t0 == 0 ? 0u : chunk + 1u;
+        if (pc.t0 == 0 && !whole) {
+            uint32_t n = 1;
+            for (size_t y = x + 1; y < pieces.size() && pieces[y].t0 > 0; ++y) ++n;
+            for (uint32_t r = 0; r < t.n_readers; ++r) {
+                const uint32_t e = t.reader_begin + r;
+                w->slots[(size_t)e * Hkv + pc.head] = (uint32_t)*n_slots;
+                merges->push_back(cart_merge_item{w->readers[e] * Hkv + pc.head, (uint32_t)*n_slots, (uint32_t)*n_slots + n, 0u});
+                *n_slots += (int32_t)n;
+            }
+        }
+        const size_t unit0 = w->units.size();
+        uint32_t at = 0;
+        for (uint32_t y = 0; y < t.n_runs; ++y) {
+            const cart_shared_unit &run = runs[t.first_run + y];
+            const uint32_t lo = std::max(at, pc.t0), hi = std::min(at + run.n_tiles, pc.t1);
+            if (lo < hi) {
+                cart_shared_unit u = run;
+                const uint32_t off = lo - at;
+                u.k_row += off * (T / (uint32_t)kTileTokens);
+                u.n_tiles = hi - lo;
+                u.v_row = pc.head;
+                u.kv_head = (uint16_t)pc.head;
+                u.lim_base -= (int32_t)(off * T);
+                u.lim_cap -= (int32_t)(off * T);
+                u.chunk = chunk;
+                u.flags |= (uint16_t)(CART_UNIT_HOLD | (w->units.size() > unit0 ? CART_UNIT_CONT : 0u));
+                // (an inner piece of a run with a ragged end does not reach that end)
+                w->units.push_back(u);
+            }
+            at += run.n_tiles;
+        }
+        w->units[unit0].reserved = (uint32_t)(w->units.size() - unit0);
+        w->units.back().flags = (uint16_t)((w->units.back().flags & ~CART_UNIT_HOLD) | (whole ? CART_UNIT_DIRECT : 0u));
+    }
+    while (block_end < first.size()) {
+        w->cta.push_back((uint32_t)w->units.size());
+        ++block_end;
+    }
+    return (int32_t)w->cta.size() - 1;
+}
+
 // Finds or makes the plan of an attention call.  n_new = null: one query per cache.
 cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t n_ids, const int32_t *n_new, bool stepping,
                       cudaStream_t s, Slot **out, int32_t *grow)
@@ -404,15 +585,26 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
     cart_status r = free_slot(ctx, st, &sl);
     if (r != CART_OK) return r;
     const Q8Layout &lay = st->lay;
-    uint32_t *list = reinterpret_cast<uint32_t *>(sl->host + lay.pages_off);
+    uint32_t *list = reinterpret_cast<uint32_t *>(sl->host);
     uint32_t n_listed = 0;
     ++st->list_stamp;
+    sl->bases.clear();
+    for (int32_t i = 0; i < n_ids; ++i) {
+        Cache &c = st->caches[(size_t)ids[i]];
+        bool room = list_pages(st, c, list, &n_listed);
+        for (int32_t q : c.parts) room = room && list_pages(st, st->caches[(size_t)q], list, &n_listed);
+        if (!room) return ctx_fail(ctx, CART_ERR_CAPACITY, "q8 attention: the batch names more than %d pages", lay.pages_cap);
+        sl->bases.push_back(c.list_base);
+    }
+    // Rows that stream their caches (single queries, and messages of a few tokens), and messages that run as chains.
     auto &segs = st->seg_tmp;
     auto &sb = st->seg_begin_tmp;
+    auto &row_of = st->row_tmp;   // query row of the stream's i-th row
     segs.clear();
     sb.assign(1, 0);
-    sl->bases.clear();
-    auto push = [&](Cache &c, int32_t n_tok, uint32_t flags) {
+    row_of.clear();
+    std::vector<Message> messages;
+    auto push = [&](const Cache &c, int32_t n_tok, uint32_t flags) {
         if (n_tok <= 0) return;
         cart_plan_seg sg;
         sg.k_row = c.list_base;
@@ -423,39 +615,116 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
         sg.flags = flags | CART_SEG_PAGED;
         segs.push_back(sg);
     };
-    int32_t n_rows = 0;
+    uint32_t n_rows = 0;
     for (int32_t i = 0; i < n_ids; ++i) {
-        Cache &c = st->caches[(size_t)ids[i]];
-        bool room = list_pages(st, c, list, &n_listed);
-        for (int32_t q : c.parts) room = room && list_pages(st, st->caches[(size_t)q], list, &n_listed);
-        if (!room) return ctx_fail(ctx, CART_ERR_CAPACITY, "q8 attention: the batch names more than %d pages", lay.pages_cap);
-        sl->bases.push_back(c.list_base);
+        const Cache &c = st->caches[(size_t)ids[i]];
         const int32_t m = n_new ? n_new[i] : 1, len = c.len[(size_t)layer];
+        if (m >= kChainRows) {
+            messages.push_back(Message{&c, n_rows, m, len});
+            n_rows += (uint32_t)m;
+            continue;
+        }
         for (int32_t r2 = 0; r2 < m; ++r2) {
             for (int32_t q : c.parts) push(st->caches[(size_t)q], st->caches[(size_t)q].len[(size_t)layer], 0);
             push(c, len - (m - 1 - r2), CART_SEG_SUFFIX);
             sb.push_back((int32_t)segs.size());
-            ++n_rows;
+            row_of.push_back(n_rows++);
         }
     }
-    cart_plan_out po{};
-    po.items = reinterpret_cast<cart_work_item *>(sl->host + lay.items_off);
-    po.items_cap = lay.items_cap;
-    po.cta_begin = reinterpret_cast<uint32_t *>(sl->host);
-    po.merges = reinterpret_cast<cart_merge_item *>(sl->host + lay.merges_off);
-    po.merges_cap = lay.merges_cap;
-    po.slots_cap = lay.slots_cap;
-    po.piece_cost = cv.piece_cost;
-    r = cart_plan_build_shared(segs.data(), sb.data(), n_rows, Hkv, cv.group, std::min(cv.n_cta, kQ8MaxCta), kTileTokens, 0,
-                               kShareTileTokens, &po);
-    if (r != CART_OK) return ctx_fail(ctx, r, "q8 attention: planning failed (%s)", cart_status_string(r));
-    sl->n_items = po.n_items;
-    sl->n_merges = po.n_merges;
-    sl->n_cta_used = po.n_cta_used;
-    Q8_CUDA(ctx, cudaMemcpyAsync(sl->dev, sl->host, lay.items_off + (uint64_t)po.n_items * sizeof(cart_work_item),
-                                 cudaMemcpyHostToDevice, s));
+    auto &items = st->item_tmp;
+    auto &merges = st->merge_tmp;
+    auto &cta = st->cta_tmp;
+    const int n_cta = std::min(cv.n_cta, kQ8MaxCta);
+    for (TileWork &w : st->work_tmp) {
+        w.units.clear();
+        w.cta.clear();
+        w.readers.clear();
+        w.slots.clear();
+    }
+    items.clear();
+    merges.clear();
+    cta.clear();
+    int32_t n_slots = 0;
+    sl->n_cta_used = 0;
+    for (auto &t : sl->tiles) t.n_cta = 0;
+    if (!row_of.empty()) {
+        TileWork &w = st->work_tmp[0];
+        // (as much as these rows can need)
+        const size_t n_rg = row_of.size() * (size_t)Hkv, n_run = segs.size() * (size_t)Hkv;
+        items.resize(2 * n_run + (size_t)n_cta + 8);
+        merges.resize(n_rg + (size_t)n_cta);
+        cta.resize((size_t)n_cta + 1);
+        w.units.resize(n_run + (size_t)n_cta);
+        w.cta.resize((size_t)n_cta + 1);
+        w.readers.resize(segs.size());
+        w.slots.resize(n_run);
+        std::vector<uint32_t> unused(n_run);  // merge item per (reader, KV head)
+        cart_plan_out po{};
+        po.items = items.data();
+        po.items_cap = (int32_t)items.size();
+        po.cta_begin = cta.data();
+        po.merges = merges.data();
+        po.merges_cap = (int32_t)merges.size();
+        po.slots_cap = lay.slots_cap;
+        po.piece_cost = cv.piece_cost;
+        po.unit_cost = cv.unit_cost;
+        po.units = w.units.data();
+        po.units_cap = (int32_t)w.units.size();
+        po.unit_cta_begin = w.cta.data();
+        po.readers = w.readers.data();
+        po.readers_cap = (int32_t)segs.size();
+        po.reader_slot = w.slots.data();
+        po.reader_merge = unused.data();
+        r = cart_plan_build_shared(segs.data(), sb.data(), (int32_t)row_of.size(), Hkv, cv.group, n_cta, kTileTokens,
+                                   cv.share_min_readers, kShareTileTokens, &po);
+        if (r != CART_OK) return ctx_fail(ctx, r, "q8 attention: planning failed (%s)", cart_status_string(r));
+        items.resize((size_t)po.n_items);
+        merges.resize((size_t)po.n_merges);
+        n_slots = po.n_slots;
+        sl->n_cta_used = po.n_items > 0 ? po.n_cta_used : 0;
+        w.units.resize((size_t)po.n_units);
+        w.readers.resize((size_t)po.n_readers);
+        w.slots.resize((size_t)po.n_readers * (size_t)Hkv);
+        w.cta.resize((size_t)po.n_unit_cta_used + 1);
+        sl->tiles[0].n_cta = po.n_units > 0 ? po.n_unit_cta_used : 0;
+        for (cart_shared_unit &u : w.units) u.reserved = 1;  // every unit brings its own rows
+        // the planner numbers the rows that it was given; here they have places among all rows
+        auto place = [&](uint32_t rg) { return row_of[rg / (uint32_t)Hkv] * (uint32_t)Hkv + rg % (uint32_t)Hkv; };
+        for (cart_work_item &it : items) it.row_group = place(it.row_group);
+        for (cart_merge_item &mi : merges) mi.row_group = place(mi.row_group);
+        for (uint32_t &x : w.readers) x = row_of[x];
+    }
+    if (!messages.empty()) {
+        sl->tiles[1].n_cta = plan_messages(st, cv, layer, messages, n_cta, lay.slots_cap, &n_slots, &merges, &st->work_tmp[1]);
+    }
+    sl->n_items = (int32_t)items.size();
+    sl->n_merges = (int32_t)merges.size();
+    // one buffer, one copy
+    uint64_t at = 0;
+    bool fits = true;
+    auto put = [&](const void *src, uint64_t bytes) {
+        const uint64_t off = at;
+        if (at + bytes > lay.slot_bytes) fits = false;
+        else if (bytes > 0 && src) std::memcpy(sl->host + at, src, bytes);
+        at += up(bytes);
+        return off;
+    };
+    (void)put(nullptr, (uint64_t)n_listed * 4);   // the page list is in place
+    sl->cta_off = put(cta.data(), cta.size() * 4);
+    sl->items_off = put(items.data(), items.size() * sizeof(cart_work_item));
+    sl->merges_off = put(merges.data(), merges.size() * sizeof(cart_merge_item));
+    for (int x = 0; x < 2; ++x) {
+        const TileWork &w = st->work_tmp[x];
+        if (sl->tiles[x].n_cta == 0) continue;
+        sl->tiles[x].cta_off = put(w.cta.data(), w.cta.size() * 4);
+        sl->tiles[x].units_off = put(w.units.data(), w.units.size() * sizeof(cart_shared_unit));
+        sl->tiles[x].readers_off = put(w.readers.data(), w.readers.size() * 4);
+        sl->tiles[x].slots_off = put(w.slots.data(), w.slots.size() * 4);
+    }
+    if (!fits || merges.size() > (size_t)lay.merges_cap)
+        return ctx_fail(ctx, CART_ERR_CAPACITY, "q8 attention: the batch's plan exceeds the tables' room");
+    Q8_CUDA(ctx, cudaMemcpyAsync(sl->dev, sl->host, std::min(at, lay.slot_bytes), cudaMemcpyHostToDevice, s));
     use_slot(st, sl, s);
-    Q8_CUDA(ctx, cudaMemcpyAsync(sl->dev + lay.pages_off, sl->host + lay.pages_off, (uint64_t)n_listed * 4, cudaMemcpyHostToDevice, s));
     sl->key = key;
     sl->lens = lens;
     sl->epoch = st->epoch;
@@ -470,32 +739,62 @@ cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t laye
     const CtxView cv = ctx_view(ctx);
     Q8State *st = *cv.q8;
     const Q8Layout &lay = st->lay;
-    Q8StreamParams p;
-    p.cta_begin = reinterpret_cast<const uint32_t *>(sl->dev);
-    p.items = reinterpret_cast<const cart_work_item *>(sl->dev + lay.items_off);
-    p.pages = reinterpret_cast<const uint32_t *>(sl->dev + lay.pages_off);
-    p.arena = static_cast<const uint8_t *>(cv.cfg->arena);
-    p.q = q;
-    p.out = out;
-    p.lse = lse;
-    p.part_o = reinterpret_cast<float *>(st->base + lay.part_o_off);
-    p.part_lse2 = reinterpret_cast<float *>(st->base + lay.part_lse_off);
-    p.merges = reinterpret_cast<const cart_merge_item *>(sl->dev + lay.merges_off);
-    const bool merge_after = sl->n_merges > cv.n_cta;
-    p.tickets = merge_after ? nullptr : reinterpret_cast<uint32_t *>(st->base);
-    p.status = cv.status;
-    p.layer = layer;
-    p.group = cv.group;
-    p.scale_log2 = cv.scale * 1.4426950408889634f;
-    p.grow = (uint32_t)grow;
+    float *part_o = reinterpret_cast<float *>(st->base + lay.part_o_off), *part_lse2 = reinterpret_cast<float *>(st->base + lay.part_lse_off);
+    const cart_merge_item *merges = reinterpret_cast<const cart_merge_item *>(sl->dev + sl->merges_off);
+    const bool tiles = sl->tiles[0].n_cta > 0 || sl->tiles[1].n_cta > 0;
+    // Partials of the tile kernel, or many: a merge kernel.  Few, all of the stream kernel: whichever block comes last merges.
+    const bool merge_after = sl->n_merges > 0 && (tiles || sl->n_merges > cv.n_cta);
+    const float scale_log2 = cv.scale * 1.4426950408889634f;
     use_slot(st, sl, s);
-    Q8_CUDA(ctx, q8_launch_stream(p, format, sl->n_cta_used, s));
-    ++*cv.launches;
+    for (const Slot::Tiles &t : sl->tiles) {
+        if (t.n_cta == 0) continue;
+        Q8TileParams p;
+        p.unit_cta_begin = reinterpret_cast<const uint32_t *>(sl->dev + t.cta_off);
+        p.units = reinterpret_cast<const cart_shared_unit *>(sl->dev + t.units_off);
+        p.readers = reinterpret_cast<const uint32_t *>(sl->dev + t.readers_off);
+        p.reader_slot = reinterpret_cast<const uint32_t *>(sl->dev + t.slots_off);
+        p.pages = reinterpret_cast<const uint32_t *>(sl->dev);
+        p.arena = static_cast<const uint8_t *>(cv.cfg->arena);
+        p.q = q;
+        p.out = out;
+        p.lse = lse;
+        p.part_o = part_o;
+        p.part_lse2 = part_lse2;
+        p.status = cv.status;
+        p.layer = layer;
+        p.group = cv.group;
+        p.n_kv_heads = cv.cfg->n_kv_heads;
+        p.n_q_heads = cv.cfg->n_q_heads;
+        p.scale_log2 = scale_log2;
+        Q8_CUDA(ctx, q8_launch_tile(p, format, t.n_cta, s));
+        ++*cv.launches;
+    }
+    if (sl->n_cta_used > 0) {
+        Q8StreamParams p;
+        p.cta_begin = reinterpret_cast<const uint32_t *>(sl->dev + sl->cta_off);
+        p.items = reinterpret_cast<const cart_work_item *>(sl->dev + sl->items_off);
+        p.pages = reinterpret_cast<const uint32_t *>(sl->dev);
+        p.arena = static_cast<const uint8_t *>(cv.cfg->arena);
+        p.q = q;
+        p.out = out;
+        p.lse = lse;
+        p.part_o = part_o;
+        p.part_lse2 = part_lse2;
+        p.merges = merges;
+        p.tickets = merge_after ? nullptr : reinterpret_cast<uint32_t *>(st->base);
+        p.status = cv.status;
+        p.layer = layer;
+        p.group = cv.group;
+        p.scale_log2 = scale_log2;
+        p.grow = (uint32_t)grow;
+        Q8_CUDA(ctx, q8_launch_stream(p, format, sl->n_cta_used, s));
+        ++*cv.launches;
+    }
     if (merge_after) {
         MergeParams mp;
-        mp.merges = p.merges;
-        mp.part_o = p.part_o;
-        mp.part_lse2 = p.part_lse2;
+        mp.merges = merges;
+        mp.part_o = part_o;
+        mp.part_lse2 = part_lse2;
         mp.out = out;
         mp.lse = lse;
         mp.group = cv.group;

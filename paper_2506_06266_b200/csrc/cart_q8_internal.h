@@ -63,7 +63,27 @@ struct Q8StreamParams {
     uint32_t grow;                   // tokens every cache has gained since the plan was built
 };
 
+struct Q8TileParams {                // the tcgen05 kernel: units as in cart_plan.h, all CART_UNIT_PAGED
+    const uint32_t *unit_cta_begin;  // [grid + 1]
+    // v_row = KV head, layer_stride = KV heads; `reserved` of a chain's first unit: how many units on the next chain
+    // begins; tr_hi of a masked unit: first reader that it belongs to << 16 | one past the last
+    const cart_shared_unit *units;
+    const uint32_t *readers;         // query row per reader entry
+    const uint32_t *reader_slot;     // [entry * Hkv + KV head]: first partial slot; + unit.chunk
+    const uint32_t *pages;
+    const uint8_t *arena;
+    const void *q;
+    void *out;
+    float *lse;
+    float *part_o, *part_lse2;
+    uint32_t *status;
+    int32_t layer, group, n_kv_heads, n_q_heads;
+    float scale_log2;
+};
+
 cudaError_t q8_prepare_kernels();
+cudaError_t q8_prepare_tile_kernels();
+cudaError_t q8_launch_tile(const Q8TileParams &p, int format, int grid, cudaStream_t s);
 cudaError_t q8_launch_write(const Q8CopyParams &p, uint32_t n_tasks, cudaStream_t s);
 cudaError_t q8_launch_read(const Q8CopyParams &p, uint32_t n_tasks, cudaStream_t s);
 cudaError_t q8_launch_stream(const Q8StreamParams &p, int format, int grid, cudaStream_t s);

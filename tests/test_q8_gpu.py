@@ -292,6 +292,122 @@ def test_messages_are_causal(pair, fmt, hq, hkv):
 
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("hq,hkv,users", [(3, 1, 90), (8, 1, 20), (10, 2, 4), (16, 2, 37)])
+def test_parts_that_many_share(pair, fmt, hq, hkv, users):
+    p = pair(hq, hkv, fmt, rows=100)
+    n = (128, 400, 1030, 127)
+    z = [p.open() for _ in n]
+    p.write(z, [rand((m, hkv, 128), m, 6) for m in n], [rand((m, hkv, 128), m + 9, 6) for m in n])
+    ids = [p.open([z[0], z[1], z[2], z[3]][i % 3:]) for i in range(users)]
+    own = [(7 * i) % 150 for i in range(users)]
+    p.write(ids, [rand((m, hkv, 128), 60 + m) for m in own], [rand((m, hkv, 128), 70 + m) for m in own])
+    q = rand((users, hq, 128), 8)
+    out, lse = p.attend_and_check(ids, q, extra=2)
+    apart = binding_without_sharing(p, ids, q)
+    assert float((apart[0].float() - out.float()).norm() / out.float().norm()) < 0.01
+    # two at a time: everyone streams
+    p.attend_and_check(ids[:2], q[:2])
+
+
+def binding_without_sharing(p, ids, q):
+    B.cart_set_share_min_readers(p.ctx, 0)
+    got = p.attend_and_check(ids, q)
+    B.cart_set_share_min_readers(p.ctx, 4)
+    return got
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("hq,hkv", [(3, 1), (5, 1), (16, 2), (4, 4)])
+@pytest.mark.parametrize("n,new,parts", [(4, 4, []), (700, 4, [1]), (130, 130, [128]), (600, 257, [300, 5]), (1500, 60, [64, 1, 900])])
+def test_one_message(pair, fmt, hq, hkv, n, new, parts):
+    p = pair(hq, hkv, fmt, rows=300)
+    z = [p.open() for _ in parts]
+    if parts:
+        p.write(z, [rand((m, hkv, 128), m) for m in parts], [rand((m, hkv, 128), m + 9) for m in parts])
+    c = p.open(z)
+    p.write([c], [rand((n, hkv, 128), 5)], [rand((n, hkv, 128), 6)])
+    p.attend_and_check([c], 2 * rand((new, hq, 128), 7), [new], extra=1)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_messages_of_several_users_among_users_that_decode(pair, fmt):
+    p = pair(8, 2, fmt, rows=500)
+    z = [p.open() for _ in range(3)]
+    p.write(z, [rand((m, 2, 128), m) for m in (300, 64, 517)], [rand((m, 2, 128), m + 9) for m in (300, 64, 517)])
+    parts = [[z[0]], [], [z[0]], [z[2], z[1]], [z[0]], [z[2], z[1]], [z[0]], [z[0]], [], [z[0]]]
+    n = [50, 4, 200, 33, 1, 129, 90, 3, 260, 8]
+    new = [50, 4, 30, 33, 1, 100, 1, 3, 140, 1]
+    ids = [p.open(x) for x in parts]
+    p.write(ids, [rand((m, 2, 128), 5 + m) for m in n], [rand((m, 2, 128), 6 + m) for m in n])
+    p.attend_and_check(ids, 2 * rand((sum(new), 8, 128), 7), new, extra=4)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("where", ["k", "v", "q"])
+def test_a_nan_in_a_message_stays_with_the_rows_that_see_it(pair, fmt, where):
+    p = pair(4, 2, fmt, rows=200)
+    z, c = p.open(), None
+    kz, vz, k, v, q = (rand(s, i) for i, s in enumerate([(140, 2, 128)] * 2 + [(150, 2, 128)] * 2 + [(150, 4, 128)]))
+    if where == "k":
+        k[100, 1, 9] = float("nan")
+    elif where == "v":
+        v[100, 1, 9] = float("-inf")
+    else:
+        q[70, 2, 100] = float("inf")
+    p.write([z], [kz], [vz])
+    c = p.open([z])
+    p.write([c], [k], [v])
+    out, lse = p.attend([c], q, [150])
+    bad, bad_l = torch.isnan(out).cpu(), torch.isnan(lse).cpu()
+    want = torch.zeros((150, 4), dtype=torch.bool)
+    if where == "q":
+        want[70, 2] = True
+    else:
+        want[96:, 2:] = True                             # the block of 16 that holds it reads as NaN
+    assert torch.equal(bad.all(-1), want) and torch.equal(bad.any(-1), want)
+    assert torch.equal(bad_l, want if where != "v" else torch.zeros_like(want))
+    # in a part that many share, and in one of its readers' queries
+    y = p.open()
+    p.write([y], [k], [v])
+    ids = [p.open([y]) for _ in range(6)]
+    out, lse = p.attend(ids, q[68:74])
+    want = torch.zeros((6, 4), dtype=torch.bool)
+    if where == "q":
+        want[2, 2] = True
+    else:
+        want[:, 2:] = True
+    assert torch.equal(torch.isnan(out).all(-1).cpu(), want) and torch.equal(torch.isnan(out).any(-1).cpu(), want)
+    assert torch.equal(torch.isnan(lse).cpu(), want if where != "v" else torch.zeros_like(want))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_messages_over_values_of_every_size(pair, fmt):
+    # large and tiny blocks, and in e4m3 codes down to the smallest, next to each other
+    p = pair(3, 1, fmt, rows=64)
+    c = p.open()
+    n = 500
+    v = (rand((n, 1, 128), 2).float() * 2.0 ** torch.linspace(-60, 60, n // 4)[torch.randperm(n // 4)].round().repeat_interleave(4)[:, None, None])
+    k = rand((n, 1, 128), 1).float() * 2.0 ** torch.linspace(-12, 0, 128).round()
+    p.write([c], [k.to(torch.bfloat16)], [v.to(torch.bfloat16)])
+    p.attend_and_check([c], 2 * rand((60, 3, 128), 3), [60])
+    p.attend_and_check([c], 30 * rand((60, 3, 128), 3), [60])
+    d = p.open()
+    p.write([d], [(k * 2.0 ** 100).to(torch.bfloat16)], [(v * 2.0 ** 50).to(torch.bfloat16)])
+    p.attend_and_check([d], (rand((60, 3, 128), 3).float() * 2.0 ** -100).to(torch.bfloat16), [60])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_a_message_behind_what_was_dropped(pair, fmt):
+    p = pair(8, 2, fmt, rows=64)
+    c = p.open()
+    k, v = rand((300, 2, 128), 1), rand((300, 2, 128), 2)
+    k[150:], v[150:] = float("nan"), float("inf")
+    p.write([c], [k], [v])
+    p.write([c], [rand((21, 2, 128), 3)], [rand((21, 2, 128), 4)], [128])
+    p.attend_and_check([c], rand((21, 8, 128), 5), [21])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 def test_what_lies_behind_a_cache_does_not_matter(pair, fmt):
     # NaN and infinities in tokens dropped by a rewind, in other blocks and (after the block was begun anew) in none
     p = pair(8, 2, fmt)
