@@ -381,6 +381,9 @@ struct Message {
 // Messages of at least this many rows run as chains of tiles on the tcgen05 kernel, shorter ones row by row on the
 // stream kernel: a tile of 128 tokens takes the one as long as the other about three rows.
 constexpr int kChainRows = 4;
+// What a row group's piece costs a block of the stream kernel, in 64-token tile times (see cart_set_piece_cost, which
+// tunes the bf16 kernel's): its warps combine once at the end, so a piece costs little.
+constexpr int kStreamPieceTiles = 1;
 // What a chain's piece costs a block beside its tiles (its rows fetched, its result written), in tile times.
 constexpr uint32_t kPieceTiles = 3;
 
@@ -565,8 +568,6 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
         lens.push_back(c.len[(size_t)layer]);
     }
     key.push_back(cv.share_min_readers);
-    key.push_back(cv.piece_cost);
-    key.push_back(cv.side_by_side);
     for (Slot &sl : st->slots) {
         if (sl.kind != (decode ? kDecode : kMessage) || sl.epoch != st->epoch || sl.key != key) continue;
         if (decode ? cart_plan_reusable(sl.lens.data(), lens.data(), n_ids, cv.max_grow, grow) != 0 : sl.lens == lens) {
@@ -666,7 +667,7 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
         po.merges = merges.data();
         po.merges_cap = (int32_t)merges.size();
         po.slots_cap = lay.slots_cap;
-        po.piece_cost = cv.piece_cost;
+        po.piece_cost = kStreamPieceTiles;
         po.unit_cost = cv.unit_cost;
         po.units = w.units.data();
         po.units_cap = (int32_t)w.units.size();

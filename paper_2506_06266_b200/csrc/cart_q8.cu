@@ -317,10 +317,10 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_read_kernel(const __grid
 
 // ---- attention that streams a cache ----------------------------------------------------------------------
 // The work list is the planner's (cart_plan.h): block c runs the items cta_begin[c] .. cta_begin[c + 1] - 1, each a run
-// of pages of one (query row, KV head).  Every warp is a stream of its own: of the blocks of 16 tokens that lie end to
-// end in the thread block's items, warp w takes every kWarps-th.  It copies them into a ring of its own in shared
-// memory (one bulk copy per block: keys, values and scales), and per block computes, for the G query heads (columns of
-// the products, G <= 8):
+// of pages of one (query row, KV head).  The blocks of 16 tokens of these items, laid end to end, are cut into kWarps
+// equal ranges, and every warp is a stream of its own: it copies its blocks into a ring of its own in shared memory (one
+// bulk copy per block: keys, values and scales), and per block computes, for the G query heads (columns of the products,
+// G <= 8):
 //
 //   S^T [16 x 8] = K [16 x 128] Q^T [128 x 8]     8 products m16n8k16, codes as fp16 (exact), q as fp16 over a power of two
 //   s = S * 2^eK * scale log2(e);  m, R: running references;  l += 2^(s - m);  w = 2^(s + eV - R)
@@ -332,20 +332,30 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_read_kernel(const __grid
 // that fp16 holds to 2^-11 wherever it matters.  That rounding is the only one on the way besides fp32 sums; the sum l
 // is taken over unrounded numbers.  References only move when outgrown by more than 2^8 (a vote per block).
 // out = O * 2^(R - m) / l.
+//
+// A warp meets few row groups, most of them cut at the ends of its range.  What it holds of a cut one it leaves in shared
+// memory (a row group that ends in its range: in a place kept for that; the one that its range ends in: where its ring
+// was), and one barrier at the kernel's end later the pieces that belong together are combined.  (Dealing the blocks of
+// every row group out to all warps and combining after each cost about 4 us per row group and block: 64 requests of
+// 2048 + 1 .. 512 tokens took 61 us, 128 suffixes of 1 .. 1024 tokens 55.)
 constexpr int kWarps = 12;
-constexpr int kStages = 4;
+constexpr int kStages = 3;
 constexpr int kStreamThreads = kWarps * 32;
 constexpr float kStep = 8.f;  // how far a value may outgrow its reference (base 2)
 constexpr uint32_t kStageStride = kQ8BlockBytes;
-constexpr uint32_t kRowStride = kHeadDim + 4;  // fp32 per (warp, head) row of the combine buffer (bank spread)
-constexpr uint32_t kOffRing = 0;
-constexpr uint32_t kOffComb = kOffRing + kWarps * kStages * kStageStride;
-constexpr uint32_t kOffStat = kOffComb + (kWarps / 2) * kMaxGroup * kRowStride * 4;  // [2][warp][head]{m, l, R}
-constexpr uint32_t kOffBars = kOffStat + 2 * kWarps * kMaxGroup * 3 * 4;
+constexpr uint32_t kRowStride = kHeadDim + 4;  // fp32 per head row of a piece (bank spread)
+constexpr uint32_t kPieceBytes = kMaxGroup * kRowStride * 4;
+constexpr uint32_t kRingBytes = kStages * kStageStride;
+static_assert(kRingBytes >= kPieceBytes, "a warp's last piece is left where its ring was");
+constexpr uint32_t kOffRing = 0;                                         // [warp]
+constexpr uint32_t kOffFirst = kOffRing + kWarps * kRingBytes;           // [warp] the piece that began before the warp's range
+constexpr uint32_t kOffStat = kOffFirst + kWarps * kPieceBytes;          // [warp][first, last][head]{m, l, R}
+constexpr uint32_t kOffEnt = kOffStat + kWarps * 2 * kMaxGroup * 3 * 4;  // [warp][first, last]: 1 + item that ends the row group, 0: none
+constexpr uint32_t kOffBars = kOffEnt + kWarps * 2 * 4;
 constexpr uint32_t kOffFlag = kOffBars + kWarps * kStages * 8;
-constexpr uint32_t kStreamSmem = kOffFlag + 16;
+constexpr uint32_t kStreamSmem = kOffFlag + 16;  // abort flag, two merge flags
 static_assert(kStreamSmem <= 232448, "shared memory budget of one sm_100 block exceeded");
-static_assert(kOffComb % 16 == 0 && kOffBars % 8 == 0, "alignment");
+static_assert(kRingBytes % 16 == 0 && kOffFirst % 16 == 0 && kOffBars % 8 == 0, "alignment");
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t policy)
 {
@@ -379,98 +389,123 @@ __device__ __forceinline__ uint4 lds128(uint32_t a)
     return v;
 }
 
-// Walks the blocks that one warp takes from the thread block's items.
-struct Cursor {
-    uint32_t it, j, n_blk;   // item, block inside it, blocks in it
-    uint32_t at;             // (blocks of the items before) mod kWarps
-};
+__device__ __forceinline__ uint32_t warp_sum(uint32_t x) { return __reduce_add_sync(0xffffffffu, x); }
 
 template <int kFmt>
 __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const Q8StreamParams p)
 {
     extern __shared__ __align__(128) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
-    float *comb = reinterpret_cast<float *>(smem + kOffComb);
-    float *stat = reinterpret_cast<float *>(smem + kOffStat);
     volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(smem + kOffFlag);
-    volatile uint32_t *merge_flag = abort_flag + 1;
+    volatile uint32_t *merge_flag = abort_flag + 1;  // [2]
+    uint32_t *ent = reinterpret_cast<uint32_t *>(smem + kOffEnt);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
     const int G = p.group;
-    const uint32_t ring = base + kOffRing + (uint32_t)warp * kStages * kStageStride;
+    const uint32_t ring = base + kOffRing + (uint32_t)warp * kRingBytes;
     auto full = [&](uint32_t s) { return base + kOffBars + ((uint32_t)warp * kStages + s) * 8u; };
     pdl_launch_dependents();
     if (lane == 0) {
         for (uint32_t s = 0; s < kStages; ++s) mbar_init(full(s), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        ent[2 * warp] = ent[2 * warp + 1] = 0u;
     }
     if (threadIdx.x == 0) *abort_flag = 0;
     __syncthreads();
 
+    // ---- the warp's range of the thread block's blocks
     const uint32_t item_begin = p.cta_begin[blockIdx.x], item_end = p.cta_begin[blockIdx.x + 1];
+    auto blocks_of = [&](const cart_work_item &w) {
+        return (w.n_tok + ((w.flags & CART_ITEM_TAIL) ? p.grow : 0u) + kQ8Block - 1) / kQ8Block;
+    };
+    auto lane_blocks = [&](uint32_t b) { return b + (uint32_t)lane < item_end ? blocks_of(p.items[b + (uint32_t)lane]) : 0u; };
+    uint32_t n_all = 0;
+    for (uint32_t b = item_begin; b < item_end; b += 32u) n_all += warp_sum(lane_blocks(b));
+    const uint32_t lo = (uint32_t)((uint64_t)n_all * (uint32_t)warp / kWarps), hi = (uint32_t)((uint64_t)n_all * ((uint32_t)warp + 1u) / kWarps);
+    uint32_t it = item_end, j = 0;   // where the range begins
+    uint32_t acc = 0;
+    for (uint32_t b = item_begin; b < item_end && lo < hi; b += 32u) {
+        const uint32_t n = lane_blocks(b);
+        uint32_t incl = n;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += y;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, acc + incl > lo);
+        if (past != 0u) {
+            const int f = __ffs((int)past) - 1;
+            it = b + (uint32_t)f;
+            j = lo - (acc + __shfl_sync(0xffffffffu, incl - n, f));
+            break;
+        }
+        acc += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    uint32_t left_blocks = hi - lo;
     pdl_wait();  // the cache's last tokens, q, out and the partial slots belong to the kernels before until they are done
     const uint64_t once = l2_evict_first_policy();
 
-    auto tokens_of = [&](const cart_work_item &w) { return w.n_tok + ((w.flags & CART_ITEM_TAIL) ? p.grow : 0u); };
-    auto first_of = [&](uint32_t at) { return ((uint32_t)warp + kWarps - at) % kWarps; };
-    // ---- the issuing side: lane 0 requests blocks in the order in which the warp will want them
-    Cursor ic{item_begin, 0u, 0u, 0u};
+    // ---- the issuing side: blocks are requested in the order in which the warp will want them
+    uint32_t i_it = it, i_j = j, i_n = 0, i_left = left_blocks;
+    uint32_t i_page0 = 0, page_lane = 0;   // lane l holds the base row of page i_page0 + l of the item
     cart_work_item iw{}, iw_next{};
-    if (item_begin < item_end) {
-        iw = p.items[item_begin];
-        if (item_begin + 1 < item_end) iw_next = p.items[item_begin + 1];
-        ic.n_blk = (tokens_of(iw) + kQ8Block - 1) / kQ8Block;
-        ic.j = first_of(0u);
+    if (i_left > 0u) {
+        iw = p.items[i_it];
+        if (i_it + 1 < item_end) iw_next = p.items[i_it + 1];
+        i_n = blocks_of(iw);
+        i_page0 = ~0u;
     }
-    uint32_t issued = 0;       // blocks requested so far
-    uint32_t page_lane = 0;    // base row of the page of the warp's (32 c + lane)-th block of the item
-    uint32_t nth = 0;          // blocks of the item requested by this warp
+    uint32_t issued = 0;
     auto issue_one = [&]() {
-        while (ic.it < item_end && ic.j >= ic.n_blk) {
-            ic.at = (ic.at + ic.n_blk) % kWarps;
-            ++ic.it;
+        if (i_left == 0u) return;
+        if (i_j == i_n) {   // (every item has a block)
+            ++i_it;
             iw = iw_next;
-            if (ic.it >= item_end) return;
-            if (ic.it + 1 < item_end) iw_next = p.items[ic.it + 1];
-            ic.n_blk = (tokens_of(iw) + kQ8Block - 1) / kQ8Block;
-            ic.j = first_of(ic.at);
-            nth = 0;
+            if (i_it + 1 < item_end) iw_next = p.items[i_it + 1];
+            i_n = blocks_of(iw);
+            i_j = 0;
+            i_page0 = ~0u;
         }
-        if (ic.it >= item_end) return;
-        if ((nth & 31u) == 0u) {
-            const uint32_t jj = ic.j + (uint32_t)lane * kWarps;
-            page_lane = jj < ic.n_blk ? __ldg(p.pages + iw.k_row + jj / (kTileTokens / kQ8Block)) : 0u;
+        const uint32_t pg = i_j / (kTileTokens / kQ8Block);
+        if (i_page0 == ~0u || pg - i_page0 >= 32u) {
+            i_page0 = pg;
+            page_lane = (pg + (uint32_t)lane) * (kTileTokens / kQ8Block) < i_n ? __ldg(p.pages + iw.k_row + pg + (uint32_t)lane) : 0u;
         }
-        const uint32_t page = __shfl_sync(0xffffffffu, page_lane, (int)(nth & 31u));
+        const uint32_t page = __shfl_sync(0xffffffffu, page_lane, (int)(pg - i_page0));
         const uint32_t s = issued % kStages;
         if (lane == 0) {
             const uint8_t *src = p.arena + (size_t)page * kRowBytes +
                                  ((size_t)((uint32_t)p.layer * iw.layer_stride + iw.v_row) * (kTileTokens / kQ8Block) +
-                                  ic.j % (kTileTokens / kQ8Block)) * kQ8BlockBytes;
+                                  i_j % (kTileTokens / kQ8Block)) * kQ8BlockBytes;
             mbar_expect_tx(full(s), kQ8BlockBytes);
             bulk_load(ring + s * kStageStride, src, kQ8BlockBytes, full(s), once);
         }
         ++issued;
-        ++nth;
-        ic.j += kWarps;
+        ++i_j;
+        --i_left;
     };
 #pragma unroll 1
     for (int s = 0; s < kStages; ++s) issue_one();
 
     // ---- the computing side
     uint32_t done = 0;            // blocks computed so far
-    uint32_t at = 0;              // as Cursor::at
     bool alive = true;
-    uint32_t piece = 0;
+    bool from_begin = false;      // the row group's first block here was the warp's
+    bool fresh = true;            // the next block starts a row group (or the range)
     uint32_t qb[8][2];            // Q^T fragments (head g)
     float f0 = 0.f, f1 = 0.f;     // scale log2(e) 2^(q's exponent) of the heads 2t, 2t + 1
     float o[8][4];                // O^T: dims 16 i + g (+ 8), heads 2t, 2t + 1
     float m0 = 0.f, m1 = 0.f, r0 = 0.f, r1 = 0.f, l0 = 0.f, l1 = 0.f;
     const float none = -INFINITY;
-    for (uint32_t it = item_begin; it < item_end; ++it) {
-        const cart_work_item w = p.items[it];
-        const uint32_t n_tok = tokens_of(w), n_blk = (n_tok + kQ8Block - 1) / kQ8Block;
-        if (w.flags & CART_ITEM_BEGIN) {
+    cart_work_item w{}, w_next{};
+    if (left_blocks > 0u) w_next = p.items[it];
+    while (left_blocks > 0u && alive) {
+        w = w_next;
+        if (it + 1 < item_end) w_next = p.items[it + 1];
+        const uint32_t n_tok = w.n_tok + ((w.flags & CART_ITEM_TAIL) ? p.grow : 0u), n_blk = (n_tok + kQ8Block - 1) / kQ8Block;
+        if (fresh) {
+            fresh = false;
+            from_begin = (w.flags & CART_ITEM_BEGIN) != 0u && j == 0u;
             m0 = m1 = r0 = r1 = none;
             l0 = l1 = 0.f;
 #pragma unroll
@@ -500,8 +535,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
             f0 = __shfl_sync(0xffffffffu, f, 8 * t);
             f1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
         }
-        for (uint32_t j = ((uint32_t)warp + kWarps - at) % kWarps; j < n_blk; j += kWarps) {
-            if (!alive) break;
+        for (; j < n_blk && left_blocks > 0u; ++j) {
             const uint32_t s = done % kStages;
             alive = __all_sync(0xffffffffu, mbar_wait(full(s), (done / kStages) & 1u, abort_flag, p.status, kStatusTimeoutConsumer));
             if (!alive) break;
@@ -565,150 +599,121 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
             const uint32_t b0 = transpose8x8(pack_f16(fast_exp2(s0 + d0), fast_exp2(s1 + d1)));
             const uint32_t b1 = transpose8x8(pack_f16(fast_exp2(s2 + d0), fast_exp2(s3 + d1)));
             // O^T += V^T w^T
+            // (codes behind the cache's end may be anything, in e4m3 a NaN: they count as zeros)
+            const bool cut = kFmt == CART_Q8_E4M3 && left < (uint32_t)kQ8Block;
+            uint32_t z0 = 0u, z1 = 0u;
+            if (cut) {
+                z0 = (2u * t < left ? 0xFFFFu : 0u) | (2u * t + 1u < left ? 0xFFFF0000u : 0u);
+                z1 = (2u * t + 8u < left ? 0xFFFFu : 0u) | (2u * t + 9u < left ? 0xFFFF0000u : 0u);
+            }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                uint4 x = lds128(blk + kQ8ValueOff + c * 512 + lane * 16);
+                const uint4 x = lds128(blk + kQ8ValueOff + c * 512 + lane * 16);
                 uint32_t a0, a1, a2, a3;
                 decode4<kFmt>(x.x, a0, a2);
                 decode4<kFmt>(x.y, a1, a3);
-                if (kFmt == CART_Q8_E4M3 && left < (uint32_t)kQ8Block) {
-                    // codes behind the cache's end may be anything, NaN included: they count as zeros
-                    const uint32_t z0 = (2u * t < left ? 0xFFFFu : 0u) | (2u * t + 1u < left ? 0xFFFF0000u : 0u);
-                    const uint32_t z1 = (2u * t + 8u < left ? 0xFFFFu : 0u) | (2u * t + 9u < left ? 0xFFFF0000u : 0u);
-                    a0 &= z0;
-                    a1 &= z0;
-                    a2 &= z1;
-                    a3 &= z1;
-                }
+                if (cut) { a0 &= z0; a1 &= z0; a2 &= z1; a3 &= z1; }
                 mma_f16(o[2 * c], a0, a1, a2, a3, b0, b1);
                 decode4<kFmt>(x.z, a0, a2);
                 decode4<kFmt>(x.w, a1, a3);
-                if (kFmt == CART_Q8_E4M3 && left < (uint32_t)kQ8Block) {
-                    const uint32_t z0 = (2u * t < left ? 0xFFFFu : 0u) | (2u * t + 1u < left ? 0xFFFF0000u : 0u);
-                    const uint32_t z1 = (2u * t + 8u < left ? 0xFFFFu : 0u) | (2u * t + 9u < left ? 0xFFFF0000u : 0u);
-                    a0 &= z0;
-                    a1 &= z0;
-                    a2 &= z1;
-                    a3 &= z1;
-                }
+                if (cut) { a0 &= z0; a1 &= z0; a2 &= z1; a3 &= z1; }
                 mma_f16(o[2 * c + 1], a0, a1, a2, a3, b0, b1);
             }
             ++done;
+            --left_blocks;
             __syncwarp();  // every lane has read the stage
             issue_one();
         }
-        at = (at + n_blk) % kWarps;
-        if (!(w.flags & CART_ITEM_END)) continue;
+        if (!alive) break;
+        const bool item_over = j == n_blk;
+        const bool to_end = item_over && (w.flags & CART_ITEM_END) != 0u;
+        if (!to_end && left_blocks > 0u) {   // the row group goes on with the next item
+            ++it;
+            j = 0;
+            continue;
+        }
 
-        // ---- the piece's end: the warps' states meet in shared memory -------------------------------------------
-        float *ml = stat + (size_t)(piece & 1u) * kWarps * kMaxGroup * 3;
-        ++piece;
+        // ---- the row group, or the range, ends here
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
             l0 += __shfl_xor_sync(0xffffffffu, l0, d);
             l1 += __shfl_xor_sync(0xffffffffu, l1, d);
         }
-        if (g == 0) {
-            float *a = ml + ((size_t)warp * kMaxGroup + 2 * t) * 3;
-            a[0] = m0;
-            a[1] = l0;
-            a[2] = r0;
-            a[3] = m1;
-            a[4] = l1;
-            a[5] = r1;
-        }
-        __syncthreads();
-        {
-            float ra = none, rb = none;  // the largest reference R of the heads 2t, 2t + 1
+        if (from_begin && to_end) {
+            // all of the thread block's share of the row group: out, or the thread block's partial
+            const float la = m0 + log2f(l0), lb = m1 + log2f(l1);
+            // (R is -inf only where every value read was NaN, and the sums are; 2^(R - m) in two factors: alone it may leave fp32)
+            const float ha = r0 == none ? 1.f : exp2f(0.5f * (r0 - m0)), hb = r1 == none ? 1.f : exp2f(0.5f * (r1 - m1));
+            const float ia = ha / l0, ib = hb / l1;
+            if (w.flags & CART_ITEM_DIRECT) {
+                __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + ((size_t)w.row_group * G + g) * kHeadDim + 2 * t;
 #pragma unroll
-            for (int x = 0; x < kWarps; ++x) {
-                ra = fmaxf(ra, ml[((size_t)x * kMaxGroup + 2 * t) * 3 + 2]);
-                rb = fmaxf(rb, ml[((size_t)x * kMaxGroup + 2 * t + 1) * 3 + 2]);
-            }
-            // (a warp that had no block of the piece holds zeros)
-            const float wa = r0 == ra ? 1.f : fast_exp2(r0 - ra), wb = r1 == rb ? 1.f : fast_exp2(r1 - rb);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                o[i][0] *= wa;
-                o[i][1] *= wb;
-                o[i][2] *= wa;
-                o[i][3] *= wb;
-            }
-            float *row = comb + (size_t)(warp % (kWarps / 2)) * kMaxGroup * kRowStride + (size_t)(2 * t) * kRowStride + g;
-            auto put = [&](bool add) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-#pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        if (2 * t + hh >= G) continue;
-                        float *d = row + hh * kRowStride + 16 * i;
-                        d[0] = add ? d[0] + o[i][hh] : o[i][hh];
-                        d[8] = add ? d[8] + o[i][2 + hh] : o[i][2 + hh];
+                for (int i = 0; i < 8; ++i) {   // to (head g, dims 16 i + 2 t, + 1), and 8 further
+                    const uint32_t x = transpose8x8(pack_bf16(o[i][0] * ha * ia, o[i][1] * hb * ib));
+                    const uint32_t y = transpose8x8(pack_bf16(o[i][2] * ha * ia, o[i][3] * hb * ib));
+                    if (g < G) {
+                        *reinterpret_cast<uint32_t *>(dst + 16 * i) = x;
+                        *reinterpret_cast<uint32_t *>(dst + 16 * i + 8) = y;
                     }
                 }
-            };
-            if (warp >= kWarps / 2) put(false);
-            __syncthreads();
-            if (warp < kWarps / 2) put(true);
-            __syncthreads();
-        }
-        const bool direct = (w.flags & CART_ITEM_DIRECT) != 0u;
-        for (int x = threadIdx.x; x < G * 32; x += kStreamThreads) {
-            const int h = x >> 5, quad = x & 31;
-            float M = none, R = none, L = 0.f;
-#pragma unroll
-            for (int v = 0; v < kWarps; ++v) {
-                M = fmaxf(M, ml[((size_t)v * kMaxGroup + h) * 3]);
-                R = fmaxf(R, ml[((size_t)v * kMaxGroup + h) * 3 + 2]);
-            }
-#pragma unroll
-            for (int v = 0; v < kWarps; ++v) {
-                const float mv = ml[((size_t)v * kMaxGroup + h) * 3], lv = ml[((size_t)v * kMaxGroup + h) * 3 + 1];
-                L += mv == M ? lv : fast_exp2(mv - M) * lv;
-            }
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int v = 0; v < kWarps / 2; ++v) {
-                const float4 b = *reinterpret_cast<const float4 *>(comb + ((size_t)v * kMaxGroup + h) * kRowStride + 4 * quad);
-                a.x += b.x;
-                a.y += b.y;
-                a.z += b.z;
-                a.w += b.w;
-            }
-            const float lse2 = M + log2f(L);
-            // (R is -inf only where every value read was NaN, and the sums are)
-            const float f = R == none ? 1.f : exp2f(0.5f * (R - M));  // (in two factors: 2^(R - M) alone may leave fp32)
-            const float f2 = f / L;
-            a.x = a.x * f * f2;
-            a.y = a.y * f * f2;
-            a.z = a.z * f * f2;
-            a.w = a.w * f * f2;
-            if (direct) {
-                const size_t orow = (size_t)w.row_group * G + h;
-                uint2 packed;
-                packed.x = pack_bf16(a.x, a.y);
-                packed.y = pack_bf16(a.z, a.w);
-                *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + orow * kHeadDim + 4 * quad) = packed;
-                if (quad == 0 && p.lse) p.lse[orow] = lse2 * 0.6931471805599453f;
+                if (g == 0 && p.lse) {
+                    if (2 * t < G) p.lse[(size_t)w.row_group * G + 2 * t] = la * 0.6931471805599453f;
+                    if (2 * t + 1 < G) p.lse[(size_t)w.row_group * G + 2 * t + 1] = lb * 0.6931471805599453f;
+                }
             } else {
-                *(reinterpret_cast<float4 *>(p.part_o + ((size_t)w.slot * G + h) * kHeadDim) + quad) = a;
-                if (quad == 0) p.part_lse2[(size_t)w.slot * kMaxGroup + h] = lse2;
+                float *dst = p.part_o + ((size_t)w.slot * G + 2 * t) * kHeadDim + g;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (2 * t < G) {
+                        dst[16 * i] = o[i][0] * ha * ia;
+                        dst[16 * i + 8] = o[i][2] * ha * ia;
+                    }
+                    if (2 * t + 1 < G) {
+                        dst[kHeadDim + 16 * i] = o[i][1] * hb * ib;
+                        dst[kHeadDim + 16 * i + 8] = o[i][3] * hb * ib;
+                    }
+                }
+                if (g == 0) {
+                    if (2 * t < G) p.part_lse2[(size_t)w.slot * kMaxGroup + 2 * t] = la;
+                    if (2 * t + 1 < G) p.part_lse2[(size_t)w.slot * kMaxGroup + 2 * t + 1] = lb;
+                }
+            }
+        } else {
+            // a piece: what began before the range is the warp's first, what the range ends in its last
+            const uint32_t last = to_end ? 0u : 1u;
+            float *dst = reinterpret_cast<float *>(smem + (last ? kOffRing + (uint32_t)warp * kRingBytes : kOffFirst + (uint32_t)warp * kPieceBytes)) +
+                         (size_t)(2 * t) * kRowStride + g;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (2 * t < G) {
+                    dst[16 * i] = o[i][0];
+                    dst[16 * i + 8] = o[i][2];
+                }
+                if (2 * t + 1 < G) {
+                    dst[kRowStride + 16 * i] = o[i][1];
+                    dst[kRowStride + 16 * i + 8] = o[i][3];
+                }
+            }
+            if (g == 0) {
+                float *a = reinterpret_cast<float *>(smem + kOffStat) + ((size_t)(2 * warp + last) * kMaxGroup + 2 * t) * 3;
+                a[0] = m0;
+                a[1] = l0;
+                a[2] = r0;
+                a[3] = m1;
+                a[4] = l1;
+                a[5] = r1;
+            }
+            if (lane == 0) {
+                // the item that ends the row group here (the same for all of its pieces)
+                uint32_t e = it;
+                while (!(p.items[e].flags & CART_ITEM_END)) ++e;
+                ent[2 * warp + last] = e + 1u;
             }
         }
-        if (!direct && p.tickets != nullptr) {
-            // a split row group: the thread block whose piece arrives last merges all pieces; nobody waits
-            __threadfence();
-            __syncthreads();
-            const cart_merge_item mi = p.merges[w.merge];
-            if (threadIdx.x == 0)
-                *merge_flag = (*abort_flag == 0u && atomicAdd(&p.tickets[w.merge], 1u) + 1u == mi.slot_end - mi.slot_begin) ? 1u : 0u;
-            __syncthreads();
-            if (*merge_flag) {
-                __threadfence();
-                merge_row_group<1, 4>(mi, G, p.part_o, p.part_lse2, p.out, p.lse, (int)threadIdx.x, kStreamThreads);
-                if (threadIdx.x == 0) p.tickets[w.merge] = 0;  // ready for the next launch
-            }
-            __syncthreads();
+        fresh = true;
+        if (item_over) {
+            ++it;
+            j = 0;
         }
     }
     if (!alive && lane == 0) {
@@ -717,6 +722,92 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
             const uint64_t t0 = global_timer_ns();
             while (!mbar_try_wait(full(u % kStages), (u / kStages) & 1u) && global_timer_ns() - t0 < kWaitLimitNs) {}
         }
+    }
+    __syncthreads();
+    if (*abort_flag != 0u) return;
+
+    // ---- pieces that belong together: one warp per (row group, head) ------------------------------------------
+    uint32_t task = 0;
+    for (int a = 0; a < 2 * kWarps; ++a) {
+        const uint32_t id = ent[a];
+        if (id == 0u) continue;
+        int b = a + 1, end = a + 1;   // [a, end): the row group's pieces (and, in between, empty entries)
+        for (; b < 2 * kWarps && (ent[b] == 0u || ent[b] == id); ++b)
+            if (ent[b] == id) end = b + 1;
+        const cart_work_item e = p.items[id - 1u];
+        for (int h = 0; h < G; ++h, ++task) {
+            if (task % kWarps != (uint32_t)warp) continue;
+            float M = none, R = none, L = 0.f;
+            const float *stat = reinterpret_cast<const float *>(smem + kOffStat) + (size_t)h * 3;
+            for (int x = a; x < end; ++x) {
+                if (ent[x] == 0u) continue;
+                M = fmaxf(M, stat[(size_t)x * kMaxGroup * 3]);
+                R = fmaxf(R, stat[(size_t)x * kMaxGroup * 3 + 2]);
+            }
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int x = a; x < end; ++x) {
+                if (ent[x] == 0u) continue;
+                const float mv = stat[(size_t)x * kMaxGroup * 3], lv = stat[(size_t)x * kMaxGroup * 3 + 1], rv = stat[(size_t)x * kMaxGroup * 3 + 2];
+                L += mv == M ? lv : fast_exp2(mv - M) * lv;
+                const float f = rv == R ? 1.f : fast_exp2(rv - R);
+                const float4 y = *reinterpret_cast<const float4 *>(
+                    smem + ((x & 1) ? kOffRing + (uint32_t)(x >> 1) * kRingBytes : kOffFirst + (uint32_t)(x >> 1) * kPieceBytes) +
+                    ((size_t)h * kRowStride + 4 * lane) * 4);
+                v.x += f * y.x;
+                v.y += f * y.y;
+                v.z += f * y.z;
+                v.w += f * y.w;
+            }
+            const float f = R == none ? 1.f : exp2f(0.5f * (R - M)), f2 = f / L;
+            v.x = v.x * f * f2;
+            v.y = v.y * f * f2;
+            v.z = v.z * f * f2;
+            v.w = v.w * f * f2;
+            const float lse2 = M + log2f(L);
+            if (e.flags & CART_ITEM_DIRECT) {
+                const size_t orow = (size_t)e.row_group * G + h;
+                uint2 packed;
+                packed.x = pack_bf16(v.x, v.y);
+                packed.y = pack_bf16(v.z, v.w);
+                *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + orow * kHeadDim + 4 * lane) = packed;
+                if (lane == 0 && p.lse) p.lse[orow] = lse2 * 0.6931471805599453f;
+            } else {
+                *(reinterpret_cast<float4 *>(p.part_o + ((size_t)e.slot * G + h) * kHeadDim) + lane) = v;
+                if (lane == 0) p.part_lse2[(size_t)e.slot * kMaxGroup + h] = lse2;
+            }
+        }
+        a = end - 1;
+    }
+
+    // ---- row groups that other thread blocks hold parts of: at most the first and the last; whoever comes last merges
+    if (p.tickets == nullptr || item_begin == item_end) return;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        uint32_t e = threadIdx.x == 0 ? item_begin : item_end - 1u;   // (a block's last item ends its last row group)
+        while (!(p.items[e].flags & CART_ITEM_END)) ++e;
+        const cart_work_item x = p.items[e];
+        bool mine = !(x.flags & CART_ITEM_DIRECT) && (threadIdx.x == 0 || e != item_begin);
+        if (mine && threadIdx.x == 1) {   // (not the row group that thread 0 has)
+            uint32_t f = item_begin;
+            while (!(p.items[f].flags & CART_ITEM_END)) ++f;
+            mine = f != e;
+        }
+        uint32_t won = 0u;
+        if (mine) {
+            const cart_merge_item mi = p.merges[x.merge];
+            if (atomicAdd(&p.tickets[x.merge], 1u) + 1u == mi.slot_end - mi.slot_begin) won = x.merge + 1u;
+        }
+        merge_flag[threadIdx.x] = won;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t won = merge_flag[k];
+        if (won == 0u) continue;
+        __threadfence();
+        merge_row_group<1, 8>(p.merges[won - 1u], G, p.part_o, p.part_lse2, p.out, p.lse, (int)threadIdx.x, kStreamThreads);
+        if (threadIdx.x == 0) p.tickets[won - 1u] = 0;  // ready for the next launch
     }
 }
 
