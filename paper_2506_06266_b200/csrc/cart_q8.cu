@@ -317,10 +317,10 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_read_kernel(const __grid
 
 // ---- attention that streams a cache ----------------------------------------------------------------------
 // The work list is the planner's (cart_plan.h): block c runs the items cta_begin[c] .. cta_begin[c + 1] - 1, each a run
-// of pages of one (query row, KV head).  The blocks of 16 tokens of these items, laid end to end, are cut into kWarps
-// equal ranges, and every warp is a stream of its own: it copies its blocks into a ring of its own in shared memory (one
-// bulk copy per block: keys, values and scales), and per block computes, for the G query heads (columns of the products,
-// G <= 8):
+// of pages of one (query row, KV head).  The steps of 32 tokens (two blocks) of these items, laid end to end, are cut into
+// kWarps equal ranges, and every warp is a stream of its own: it copies its steps into a ring of its own in shared
+// memory (one bulk copy per step: keys, values and scales), and per block computes, for the G query heads (columns of
+// the products, G <= 8):
 //
 //   S^T [16 x 8] = K [16 x 128] Q^T [128 x 8]     8 products m16n8k16, codes as fp16 (exact), q as fp16 over a power of two
 //   s = S * 2^eK * scale log2(e);  m, R: running references;  l += 2^(s - m);  w = 2^(s + eV - R)
@@ -330,7 +330,8 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_read_kernel(const __grid
 // The values' scales join the exponent instead of multiplying codes or probabilities: w = p * 2^eV is held relative to
 // the largest such product (reference R, apart from the softmax's own reference m), so it is a number of at most 2^8
 // that fp16 holds to 2^-11 wherever it matters.  That rounding is the only one on the way besides fp32 sums; the sum l
-// is taken over unrounded numbers.  References only move when outgrown by more than 2^8 (a vote per block).
+// is taken over unrounded numbers.  References only move when outgrown by more than 2^8 (a vote per step).
+// (With a step of one block the waiting, requesting and voting were half of the instructions.)
 // out = O * 2^(R - m) / l.
 //
 // A warp meets few row groups, most of them cut at the ends of its range.  What it holds of a cut one it leaves in shared
@@ -338,13 +339,13 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_read_kernel(const __grid
 // was), and one barrier at the kernel's end later the pieces that belong together are combined.  (Dealing the blocks of
 // every row group out to all warps and combining after each cost about 4 us per row group and block: 64 requests of
 // 2048 + 1 .. 512 tokens took 61 us, 128 suffixes of 1 .. 1024 tokens 55.)
-constexpr int kWarps = 12;
+constexpr int kWarps = 8;
 constexpr int kStages = 3;
 constexpr int kStreamThreads = kWarps * 32;
-constexpr float kStep = 8.f;  // how far a value may outgrow its reference (base 2)
-constexpr uint32_t kStageStride = kQ8BlockBytes;
-constexpr uint32_t kRowStride = kHeadDim + 4;  // fp32 per head row of a piece (bank spread)
-constexpr uint32_t kPieceBytes = kMaxGroup * kRowStride * 4;
+constexpr float kStepUp = 8.f;                           // how far a value may outgrow its reference (base 2)
+constexpr uint32_t kStepTokens = 2 * kQ8Block;           // a warp's step: two blocks of a page
+constexpr uint32_t kStageStride = 2 * kQ8BlockBytes;
+constexpr uint32_t kPieceBytes = kMaxGroup * kHeadDim * 4;
 constexpr uint32_t kRingBytes = kStages * kStageStride;
 static_assert(kRingBytes >= kPieceBytes, "a warp's last piece is left where its ring was");
 constexpr uint32_t kOffRing = 0;                                         // [warp]
@@ -356,6 +357,7 @@ constexpr uint32_t kOffFlag = kOffBars + kWarps * kStages * 8;
 constexpr uint32_t kStreamSmem = kOffFlag + 16;  // abort flag, two merge flags
 static_assert(kStreamSmem <= 232448, "shared memory budget of one sm_100 block exceeded");
 static_assert(kRingBytes % 16 == 0 && kOffFirst % 16 == 0 && kOffBars % 8 == 0, "alignment");
+// A piece in shared memory: fp32 [head][128], dims in the order d ^ 8 (head / 2), which spreads the banks.
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t policy)
 {
@@ -413,19 +415,18 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
     if (threadIdx.x == 0) *abort_flag = 0;
     __syncthreads();
 
-    // ---- the warp's range of the thread block's blocks
+    // ---- the warp's range of the thread block's steps
     const uint32_t item_begin = p.cta_begin[blockIdx.x], item_end = p.cta_begin[blockIdx.x + 1];
-    auto blocks_of = [&](const cart_work_item &w) {
-        return (w.n_tok + ((w.flags & CART_ITEM_TAIL) ? p.grow : 0u) + kQ8Block - 1) / kQ8Block;
-    };
-    auto lane_blocks = [&](uint32_t b) { return b + (uint32_t)lane < item_end ? blocks_of(p.items[b + (uint32_t)lane]) : 0u; };
+    auto tokens_of = [&](const cart_work_item &w) { return w.n_tok + ((w.flags & CART_ITEM_TAIL) ? p.grow : 0u); };
+    auto steps_of = [&](const cart_work_item &w) { return (tokens_of(w) + kStepTokens - 1) / kStepTokens; };
+    auto lane_steps = [&](uint32_t b) { return b + (uint32_t)lane < item_end ? steps_of(p.items[b + (uint32_t)lane]) : 0u; };
     uint32_t n_all = 0;
-    for (uint32_t b = item_begin; b < item_end; b += 32u) n_all += warp_sum(lane_blocks(b));
+    for (uint32_t b = item_begin; b < item_end; b += 32u) n_all += warp_sum(lane_steps(b));
     const uint32_t lo = (uint32_t)((uint64_t)n_all * (uint32_t)warp / kWarps), hi = (uint32_t)((uint64_t)n_all * ((uint32_t)warp + 1u) / kWarps);
     uint32_t it = item_end, j = 0;   // where the range begins
     uint32_t acc = 0;
     for (uint32_t b = item_begin; b < item_end && lo < hi; b += 32u) {
-        const uint32_t n = lane_blocks(b);
+        const uint32_t n = lane_steps(b);
         uint32_t incl = n;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -441,68 +442,71 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
         }
         acc += __shfl_sync(0xffffffffu, incl, 31);
     }
-    uint32_t left_blocks = hi - lo;
+    uint32_t left_steps = hi - lo;
     pdl_wait();  // the cache's last tokens, q, out and the partial slots belong to the kernels before until they are done
     const uint64_t once = l2_evict_first_policy();
 
-    // ---- the issuing side: blocks are requested in the order in which the warp will want them
-    uint32_t i_it = it, i_j = j, i_n = 0, i_left = left_blocks;
-    uint32_t i_page0 = 0, page_lane = 0;   // lane l holds the base row of page i_page0 + l of the item
+    // ---- the issuing side: steps are requested in the order in which the warp will want them
+    uint32_t i_it = it, i_j = j, i_tok = 0, i_left = left_steps, i_slot = 0;
+    uint32_t i_page0 = 1u << 31, page_lane = 0;   // lane l holds the base row of page i_page0 + l of the item
+    const uint8_t *i_head = nullptr;         // the KV head inside a page at row 0
     cart_work_item iw{}, iw_next{};
+    auto i_item = [&]() {
+        i_tok = tokens_of(iw);
+        i_head = p.arena + (size_t)((uint32_t)p.layer * iw.layer_stride + iw.v_row) * kQ8HeadBytes;
+        i_page0 = 1u << 31;   // (further than 32 from any page)
+    };
     if (i_left > 0u) {
         iw = p.items[i_it];
         if (i_it + 1 < item_end) iw_next = p.items[i_it + 1];
-        i_n = blocks_of(iw);
-        i_page0 = ~0u;
+        i_item();
     }
-    uint32_t issued = 0;
     auto issue_one = [&]() {
         if (i_left == 0u) return;
-        if (i_j == i_n) {   // (every item has a block)
+        if (i_j * kStepTokens >= i_tok) {   // (every item has a step)
             ++i_it;
             iw = iw_next;
             if (i_it + 1 < item_end) iw_next = p.items[i_it + 1];
-            i_n = blocks_of(iw);
             i_j = 0;
-            i_page0 = ~0u;
+            i_item();
         }
-        const uint32_t pg = i_j / (kTileTokens / kQ8Block);
-        if (i_page0 == ~0u || pg - i_page0 >= 32u) {
+        const uint32_t pg = i_j >> 1;
+        if (pg - i_page0 >= 32u) {
             i_page0 = pg;
-            page_lane = (pg + (uint32_t)lane) * (kTileTokens / kQ8Block) < i_n ? __ldg(p.pages + iw.k_row + pg + (uint32_t)lane) : 0u;
+            page_lane = (pg + (uint32_t)lane) * (uint32_t)kTileTokens < i_tok ? __ldg(p.pages + iw.k_row + pg + (uint32_t)lane) : 0u;
         }
         const uint32_t page = __shfl_sync(0xffffffffu, page_lane, (int)(pg - i_page0));
-        const uint32_t s = issued % kStages;
         if (lane == 0) {
-            const uint8_t *src = p.arena + (size_t)page * kRowBytes +
-                                 ((size_t)((uint32_t)p.layer * iw.layer_stride + iw.v_row) * (kTileTokens / kQ8Block) +
-                                  i_j % (kTileTokens / kQ8Block)) * kQ8BlockBytes;
-            mbar_expect_tx(full(s), kQ8BlockBytes);
-            bulk_load(ring + s * kStageStride, src, kQ8BlockBytes, full(s), once);
+            // (only what holds tokens: the second block of the last step may be empty)
+            const uint32_t bytes = i_tok - i_j * kStepTokens > (uint32_t)kQ8Block ? 2u * kQ8BlockBytes : kQ8BlockBytes;
+            const uint32_t bar = full(i_slot);
+            mbar_expect_tx(bar, bytes);
+            bulk_load(ring + i_slot * kStageStride, i_head + (size_t)page * kRowBytes + (i_j & 1u) * kStageStride, bytes, bar, once);
         }
-        ++issued;
+        i_slot = i_slot + 1u == kStages ? 0u : i_slot + 1u;
         ++i_j;
         --i_left;
     };
+    static_assert(kTileTokens == 2 * kStepTokens, "a page is two steps");
 #pragma unroll 1
     for (int s = 0; s < kStages; ++s) issue_one();
 
     // ---- the computing side
-    uint32_t done = 0;            // blocks computed so far
+    uint32_t slot = 0, phase = 0;  // the ring's next stage, and the parity of its barrier
     bool alive = true;
-    bool from_begin = false;      // the row group's first block here was the warp's
-    bool fresh = true;            // the next block starts a row group (or the range)
+    bool from_begin = false;      // the row group's first step here was the warp's
+    bool fresh = true;            // the next step starts a row group (or the range)
     uint32_t qb[8][2];            // Q^T fragments (head g)
     float f0 = 0.f, f1 = 0.f;     // scale log2(e) 2^(q's exponent) of the heads 2t, 2t + 1
     float o[8][4];                // O^T: dims 16 i + g (+ 8), heads 2t, 2t + 1
-    float m0 = 0.f, m1 = 0.f, r0 = 0.f, r1 = 0.f, l0 = 0.f, l1 = 0.f;
     const float none = -INFINITY;
+    float m0 = none, m1 = none, r0 = none, r1 = none, l0 = 0.f, l1 = 0.f;
     cart_work_item w{}, w_next{};
-    if (left_blocks > 0u) w_next = p.items[it];
-    while (left_blocks > 0u && alive) {
+    if (left_steps > 0u) w_next = p.items[it];
+    while (left_steps > 0u && alive) {
         w = w_next;
         if (it + 1 < item_end) w_next = p.items[it + 1];
-        const uint32_t n_tok = w.n_tok + ((w.flags & CART_ITEM_TAIL) ? p.grow : 0u), n_blk = (n_tok + kQ8Block - 1) / kQ8Block;
+        const uint32_t n_tok = tokens_of(w), n_step = (n_tok + kStepTokens - 1) / kStepTokens;
         if (fresh) {
             fresh = false;
             from_begin = (w.flags & CART_ITEM_BEGIN) != 0u && j == 0u;
@@ -535,49 +539,71 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
             f0 = __shfl_sync(0xffffffffu, f, 8 * t);
             f1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
         }
-        for (; j < n_blk && left_blocks > 0u; ++j) {
-            const uint32_t s = done % kStages;
-            alive = __all_sync(0xffffffffu, mbar_wait(full(s), (done / kStages) & 1u, abort_flag, p.status, kStatusTimeoutConsumer));
+        // how many steps of the item are the warp's
+        const uint32_t stop = left_steps < n_step - j ? j + left_steps : n_step;
+        left_steps -= stop - j;
+        for (; j < stop; ++j) {
+            alive = __all_sync(0xffffffffu, mbar_wait(full(slot), phase, abort_flag, p.status, kStatusTimeoutConsumer));
             if (!alive) break;
-            const uint32_t blk = ring + s * kStageStride;
-            uint32_t scales;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(scales) : "r"(blk + kQ8ScaleOff));
-            const uint32_t ek = scales & 0xFFu, ev = scales >> 8;
-            const float nan = __uint_as_float(0x7FC00000u);
-            const float kf = ek == kQ8NoScale ? nan : exp2_int((int)ek - 127);
-            const float vx = ev == kQ8NoScale ? nan : (float)((int)ev - 127);
-            // S^T = K Q^T (two accumulators, so that the products do not wait for one another)
-            float sa[4] = {0.f, 0.f, 0.f, 0.f}, sb[4] = {0.f, 0.f, 0.f, 0.f};
+            const uint32_t stage = ring + slot * kStageStride + (uint32_t)lane * 16u;
+            const uint32_t left = n_tok - j * kStepTokens;
+            const bool two = left > (uint32_t)kQ8Block;
+            float s[2][4];
+            float vx[2];
+            // S^T = K Q^T of both blocks (what lies in place of a missing second block is masked like all behind the end)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const uint4 x = lds128(blk + c * 512 + lane * 16);
-                uint32_t a0, a1, a2, a3;
-                decode4<kFmt>(x.x, a0, a2);
-                decode4<kFmt>(x.y, a1, a3);
-                mma_f16(sa, a0, a1, a2, a3, qb[2 * c][0], qb[2 * c][1]);
-                decode4<kFmt>(x.z, a0, a2);
-                decode4<kFmt>(x.w, a1, a3);
-                mma_f16(sb, a0, a1, a2, a3, qb[2 * c + 1][0], qb[2 * c + 1][1]);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const uint4 x = lds128(stage + b * kQ8BlockBytes + c * 512);
+                    uint32_t a0, a1, a2, a3;
+                    decode4<kFmt>(x.x, a0, a2);
+                    decode4<kFmt>(x.y, a1, a3);
+                    mma_f16(s[b], a0, a1, a2, a3, qb[2 * c][0], qb[2 * c][1]);
+                    decode4<kFmt>(x.z, a0, a2);
+                    decode4<kFmt>(x.w, a1, a3);
+                    mma_f16(s[b], a0, a1, a2, a3, qb[2 * c + 1][0], qb[2 * c + 1][1]);
+                }
             }
-            const float k0 = f0 * kf, k1 = f1 * kf;
-            float s0 = (sa[0] + sb[0]) * k0, s1 = (sa[1] + sb[1]) * k1;  // token g, heads 2t and 2t + 1
-            float s2 = (sa[2] + sb[2]) * k0, s3 = (sa[3] + sb[3]) * k1;  // token g + 8
-            const uint32_t left = n_tok - j * kQ8Block;
-            if (left < (uint32_t)kQ8Block) {  // the cache ends inside the block
-                if ((uint32_t)g >= left) s0 = s1 = none;
-                if ((uint32_t)g + 8u >= left) s2 = s3 = none;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                uint32_t scales;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=r"(scales) : "r"(ring + slot * kStageStride + b * kQ8BlockBytes + kQ8ScaleOff));
+                const uint32_t ek = scales & 0xFFu, ev = scales >> 8;
+                const float nan = __uint_as_float(0x7FC00000u);
+                const float kf = ek == kQ8NoScale ? nan : __uint_as_float(ek << 23);
+                vx[b] = ev == kQ8NoScale ? nan : (float)((int)ev - 127);
+                const float k0 = f0 * kf, k1 = f1 * kf;
+                s[b][0] *= k0;   // token g, heads 2t and 2t + 1
+                s[b][1] *= k1;
+                s[b][2] *= k0;   // token g + 8
+                s[b][3] *= k1;
             }
-            const float mx0 = fmaxf(s0, s2), mx1 = fmaxf(s1, s3);
-            const bool far = mx0 > m0 + kStep || mx1 > m1 + kStep || mx0 + vx > r0 + kStep || mx1 + vx > r1 + kStep;
+            if (left < kStepTokens) {  // the cache ends inside the step
+                if (!two) vx[1] = vx[0];
+#pragma unroll
+                for (uint32_t b = 0; b < 2; ++b) {
+                    if ((uint32_t)g + 16u * b >= left) s[b][0] = s[b][1] = none;
+                    if ((uint32_t)g + 16u * b + 8u >= left) s[b][2] = s[b][3] = none;
+                }
+            }
+            const float x0 = fmaxf(s[0][0], s[0][2]), x1 = fmaxf(s[0][1], s[0][3]), y0 = fmaxf(s[1][0], s[1][2]), y1 = fmaxf(s[1][1], s[1][3]);
+            const float mx0 = fmaxf(x0, y0), mx1 = fmaxf(x1, y1);
+            const float rx0 = fmaxf(x0 + vx[0], y0 + vx[1]), rx1 = fmaxf(x1 + vx[0], y1 + vx[1]);
+            const bool far = mx0 > m0 + kStepUp || mx1 > m1 + kStepUp || rx0 > r0 + kStepUp || rx1 > r1 + kStepUp;
             if (__any_sync(0xffffffffu, far)) {
-                float c0 = mx0, c1 = mx1;
+                float c0 = mx0, c1 = mx1, c2 = rx0, c3 = rx1;
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) {
                     c0 = fmaxf(c0, __shfl_xor_sync(0xffffffffu, c0, d));
                     c1 = fmaxf(c1, __shfl_xor_sync(0xffffffffu, c1, d));
+                    c2 = fmaxf(c2, __shfl_xor_sync(0xffffffffu, c2, d));
+                    c3 = fmaxf(c3, __shfl_xor_sync(0xffffffffu, c3, d));
                 }
                 // (a NaN takes no part in a maximum; it stays in the sums)
-                const float n0 = fmaxf(m0, c0), n1 = fmaxf(m1, c1), q0 = fmaxf(r0, c0 + vx), q1 = fmaxf(r1, c1 + vx);
+                const float n0 = fmaxf(m0, c0), n1 = fmaxf(m1, c1), q0 = fmaxf(r0, c2), q1 = fmaxf(r1, c3);
                 l0 *= n0 == none ? 1.f : fast_exp2(m0 - n0);
                 l1 *= n1 == none ? 1.f : fast_exp2(m1 - n1);
                 const float a0 = q0 == none ? 1.f : fast_exp2(r0 - q0), a1 = q1 == none ? 1.f : fast_exp2(r1 - q1);
@@ -593,41 +619,56 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
                     o[i][3] *= a1;
                 }
             }
-            l0 += fast_exp2(s0 - m0) + fast_exp2(s2 - m0);
-            l1 += fast_exp2(s1 - m1) + fast_exp2(s3 - m1);
-            const float d0 = vx - r0, d1 = vx - r1;
-            const uint32_t b0 = transpose8x8(pack_f16(fast_exp2(s0 + d0), fast_exp2(s1 + d1)));
-            const uint32_t b1 = transpose8x8(pack_f16(fast_exp2(s2 + d0), fast_exp2(s3 + d1)));
-            // O^T += V^T w^T
-            // (codes behind the cache's end may be anything, in e4m3 a NaN: they count as zeros)
-            const bool cut = kFmt == CART_Q8_E4M3 && left < (uint32_t)kQ8Block;
-            uint32_t z0 = 0u, z1 = 0u;
-            if (cut) {
-                z0 = (2u * t < left ? 0xFFFFu : 0u) | (2u * t + 1u < left ? 0xFFFF0000u : 0u);
-                z1 = (2u * t + 8u < left ? 0xFFFFu : 0u) | (2u * t + 9u < left ? 0xFFFF0000u : 0u);
-            }
+            uint32_t pb[2][2];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint4 x = lds128(blk + kQ8ValueOff + c * 512 + lane * 16);
-                uint32_t a0, a1, a2, a3;
-                decode4<kFmt>(x.x, a0, a2);
-                decode4<kFmt>(x.y, a1, a3);
-                if (cut) { a0 &= z0; a1 &= z0; a2 &= z1; a3 &= z1; }
-                mma_f16(o[2 * c], a0, a1, a2, a3, b0, b1);
-                decode4<kFmt>(x.z, a0, a2);
-                decode4<kFmt>(x.w, a1, a3);
-                if (cut) { a0 &= z0; a1 &= z0; a2 &= z1; a3 &= z1; }
-                mma_f16(o[2 * c + 1], a0, a1, a2, a3, b0, b1);
+            for (int b = 0; b < 2; ++b) {
+                l0 += fast_exp2(s[b][0] - m0) + fast_exp2(s[b][2] - m0);
+                l1 += fast_exp2(s[b][1] - m1) + fast_exp2(s[b][3] - m1);
+                const float d0 = vx[b] - r0, d1 = vx[b] - r1;
+                pb[b][0] = transpose8x8(pack_f16(fast_exp2(s[b][0] + d0), fast_exp2(s[b][1] + d1)));
+                pb[b][1] = transpose8x8(pack_f16(fast_exp2(s[b][2] + d0), fast_exp2(s[b][3] + d1)));
             }
-            ++done;
-            --left_blocks;
+            // O^T += V^T w^T
+            auto values = [&](int b, bool cut) {
+                // (codes behind the cache's end may be anything, in e4m3 a NaN: they count as zeros)
+                uint32_t z0 = 0u, z1 = 0u;
+                if (cut) {
+                    const uint32_t u = 16u * b + 2u * t;
+                    z0 = (u < left ? 0xFFFFu : 0u) | (u + 1u < left ? 0xFFFF0000u : 0u);
+                    z1 = (u + 8u < left ? 0xFFFFu : 0u) | (u + 9u < left ? 0xFFFF0000u : 0u);
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint4 x = lds128(stage + b * kQ8BlockBytes + kQ8ValueOff + c * 512);
+                    uint32_t a0, a1, a2, a3;
+                    decode4<kFmt>(x.x, a0, a2);
+                    decode4<kFmt>(x.y, a1, a3);
+                    if (cut) { a0 &= z0; a1 &= z0; a2 &= z1; a3 &= z1; }
+                    mma_f16(o[2 * c], a0, a1, a2, a3, pb[b][0], pb[b][1]);
+                    decode4<kFmt>(x.z, a0, a2);
+                    decode4<kFmt>(x.w, a1, a3);
+                    if (cut) { a0 &= z0; a1 &= z0; a2 &= z1; a3 &= z1; }
+                    mma_f16(o[2 * c + 1], a0, a1, a2, a3, pb[b][0], pb[b][1]);
+                }
+            };
+            if (left >= kStepTokens) {
+                values(0, false);
+                values(1, false);
+            } else {
+                values(0, true);
+                if (two) values(1, true);
+            }
             __syncwarp();  // every lane has read the stage
             issue_one();
+            if (++slot == kStages) {
+                slot = 0;
+                phase ^= 1u;
+            }
         }
         if (!alive) break;
-        const bool item_over = j == n_blk;
+        const bool item_over = j == n_step;
         const bool to_end = item_over && (w.flags & CART_ITEM_END) != 0u;
-        if (!to_end && left_blocks > 0u) {   // the row group goes on with the next item
+        if (!to_end && left_steps > 0u) {   // the row group goes on with the next item
             ++it;
             j = 0;
             continue;
@@ -682,16 +723,17 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
             // a piece: what began before the range is the warp's first, what the range ends in its last
             const uint32_t last = to_end ? 0u : 1u;
             float *dst = reinterpret_cast<float *>(smem + (last ? kOffRing + (uint32_t)warp * kRingBytes : kOffFirst + (uint32_t)warp * kPieceBytes)) +
-                         (size_t)(2 * t) * kRowStride + g;
+                         (size_t)(2 * t) * kHeadDim;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+                const int d = (16 * i + g) ^ (8 * t), d8 = (16 * i + 8 + g) ^ (8 * t);
                 if (2 * t < G) {
-                    dst[16 * i] = o[i][0];
-                    dst[16 * i + 8] = o[i][2];
+                    dst[d] = o[i][0];
+                    dst[d8] = o[i][2];
                 }
                 if (2 * t + 1 < G) {
-                    dst[kRowStride + 16 * i] = o[i][1];
-                    dst[kRowStride + 16 * i + 8] = o[i][3];
+                    dst[kHeadDim + d] = o[i][1];
+                    dst[kHeadDim + d8] = o[i][3];
                 }
             }
             if (g == 0) {
@@ -717,10 +759,15 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
         }
     }
     if (!alive && lane == 0) {
-        // gave up: wait (bounded) for the copies still in flight before the thread block leaves
-        for (uint32_t u = done; u < issued; ++u) {
+        // gave up: wait (bounded) for the copies still in flight before the thread block leaves (a stage that nothing was
+        // requested for has an open barrier, which only costs the bound)
+        for (int u = 0; u < kStages; ++u) {
             const uint64_t t0 = global_timer_ns();
-            while (!mbar_try_wait(full(u % kStages), (u / kStages) & 1u) && global_timer_ns() - t0 < kWaitLimitNs) {}
+            while (!mbar_try_wait(full(slot), phase) && global_timer_ns() - t0 < kWaitLimitNs) {}
+            if (++slot == kStages) {
+                slot = 0;
+                phase ^= 1u;
+            }
         }
     }
     __syncthreads();
@@ -752,7 +799,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
                 const float f = rv == R ? 1.f : fast_exp2(rv - R);
                 const float4 y = *reinterpret_cast<const float4 *>(
                     smem + ((x & 1) ? kOffRing + (uint32_t)(x >> 1) * kRingBytes : kOffFirst + (uint32_t)(x >> 1) * kPieceBytes) +
-                    ((size_t)h * kRowStride + 4 * lane) * 4);
+                    ((size_t)h * kHeadDim + ((4 * lane) ^ (8 * (h >> 1)))) * 4);
                 v.x += f * y.x;
                 v.y += f * y.y;
                 v.z += f * y.z;
