@@ -395,7 +395,7 @@ constexpr uint32_t kPieceTiles = 3;
 int32_t plan_messages(const Q8State *st, const CtxView &cv, int32_t layer, std::vector<Message> &messages, int n_cta, int32_t slots_cap,
                       int32_t *n_slots, std::vector<cart_merge_item> *merges, TileWork *w)
 {
-    const uint32_t Hkv = (uint32_t)cv.cfg->n_kv_heads, tpt = 128u / (uint32_t)cv.group;
+    const uint32_t Hkv = (uint32_t)cv.cfg->n_kv_heads, tpt = 2u * (128u / (uint32_t)cv.group);   // two M-tiles
     std::stable_sort(messages.begin(), messages.end(), [](const Message &a, const Message &b) { return a.c->parts < b.c->parts; });
     // the runs of every M-tile (the same for all KV heads): units without their KV head, and how many tiles they have
     struct Tile { uint32_t reader_begin, n_readers, first_run, n_runs, n_tiles; };

@@ -1,20 +1,34 @@
 // Attention over caches in 8 bits for many query rows at once, on the tcgen05 tensor cores (sm_100a): parts that
 // several rows of a batch share, and messages (rows that attend causally).
 //
-// The unit of work is the shared-segment kernel's (cart_shared.cu, cart_plan.h): up to 128 query rows (the G heads of up
-// to 128 / G rows of the batch) against a run of 128-token tiles, with the same two products per tile, the same softmax
-// in two warpgroups that each own half of a tile's tokens, and the same chains.  What differs is where the operands come
-// from.  A tile is 32 KB of codes that have to become 64 KB of bf16 in shared memory:
+// A unit of work is up to 256 query rows of one KV head -- two M-tiles of 128, row i * G + h of an M-tile being head h of
+// its i-th reader -- against a run of 128-token tiles of one cache (cart_shared_unit, cart_plan.h); units that continue
+// one another form a chain, over which the rows' softmax state carries on.  Per tile and M-tile: S = Q K^T, P = 2^(s - m),
+// O += P V, all three in tensor memory (P over the scores it came from).
 //
-//   4 converter warps  each takes two blocks of 16 tokens of every tile, keys and values: 16-byte loads from global
-//                      memory (a lane's bytes of the stored order), codes to bf16, times the block's power of two (exact),
-//                      8-byte stores into the swizzled operand tiles.  The next block's loads are in flight meanwhile.
-//                      No raw tile is staged in shared memory: its bandwidth is what the products need.
-//   MMA warp           S = Q K^T as ever; O_x += P_x V_x with V as a K-major operand [dim][token], because a word of the
-//                      stored values holds four tokens of one dim.  Inside a block of 16 the tokens stand in the stored
-//                      order 0 1 8 9  2 3 10 11  4 5 12 13  6 7 14 15; the softmax threads pack their probabilities in
-//                      that order too, which costs nothing.
+//   4 converter warps  A tile is 32 KB of codes that become 64 KB of operands in shared memory.  Each warp takes two
+//                      blocks of 16 tokens of every tile, keys and values: 16-byte loads from global memory (a lane's
+//                      bytes of the stored order), codes to fp16 (keys) or bf16 (values), both exact and without the
+//                      blocks' scales, 8-byte stores into the swizzled tiles.  The next loads are in flight meanwhile.
+//                      No raw tile is staged in shared memory: its bandwidth is what the products need (per tile and
+//                      pair of M-tiles 192 KB of operands are read and 64 KB written, as long as the products take).
+//   MMA warp           one thread issues, in turns, P V of one M-tile and the next S of the same, so that one M-tile's
+//                      products run while the other's softmax does.  V is a K-major operand [dim][token], because a word
+//                      of the stored values holds four tokens of one dim; inside a block of 16 the tokens stand in the
+//                      stored order 0 1 8 9  2 3 10 11  4 5 12 13  6 7 14 15, and the softmax threads pack their
+//                      probabilities in that order, which costs nothing.
+//   2 x 4 softmax      one warpgroup per M-tile, one thread per row.  The scores are read twice from tensor memory (for
+//   warps              the maximum, then for the exponentials), which leaves the registers to the converters.  A row's
+//                      reference m moves only when outgrown by more than 2^8; its thread then rescales the accumulator.
 //
+// The scales join the softmax, where a block's 16 tokens are 16 columns of a thread's row: keys' scales multiply the
+// scores (in place of the softmax's own factor), values' scales are added in the exponent, so that P is held times the
+// scale of its values -- in bf16, whose range is fp32's -- and the sum is taken per block and freed of the scale again.
+// (Blocks beyond 2^+-60 have their codes scaled to there by the converters.)  The query rows are fp16 numbers over a
+// power of two of their own.
+//
+// Two M-tiles per converted tile halve the conversions per product: with one (the layout of cart_shared.cu, each softmax
+// warpgroup on half of a tile's tokens) a tile took 3.7 us, the converters' loads setting the pace.
 // A block of values without a scale (a NaN was written into it) becomes zeros in the operand, since rows that do not see
 // it would otherwise catch its NaN through 0 * NaN; the rows that do see one of its tokens are marked and end as NaN.
 // Every wait is bounded, as in cart_shared.cu.
@@ -33,50 +47,149 @@ constexpr uint32_t kBlock = 128u * 128u;              // 128 rows x 128 bytes: o
 constexpr uint32_t kTileBytes = 2u * kBlock;          // 128 x 128 bf16
 constexpr int kKStages = 3;
 constexpr int kVStages = 2;
-constexpr int kSBufs = 2;                             // score buffers in tensor memory
-constexpr int kThreads = 512;                         // utility warpgroup (warp 1: MMA), 2 softmax warpgroups, converters
 constexpr int kConvWarps = 4;
+constexpr int kThreads = 512;                         // utility warpgroup (warp 0: MMA), 2 softmax warpgroups, converters
 // Registers per thread after the warpgroups have re-divided the launch's 512 x 128 = 65536:
-// 128 x 32 + 256 x 192 + 128 x 96 = 65536.
-constexpr int kRegsUtility = 32;
-constexpr int kRegsSoftmax = 192;
-constexpr int kRegsConvert = 96;
-constexpr int kSoftmaxThreads = 128;                  // one softmax warpgroup
-constexpr uint32_t kTmemCols = 512;                   // S0 S1 (scores, then P), O_a O_b: 128 fp32 columns each
+// 128 x 72 + 256 x 144 + 128 x 152 = 65536.
+constexpr int kRegsUtility = 72;
+constexpr int kRegsSoftmax = 144;
+constexpr int kRegsConvert = 152;
+constexpr uint32_t kTmemCols = 512;                   // S_A S_B (scores, then P), O_A O_B: 128 fp32 columns each
 constexpr uint32_t kTmemO = 2u * 128u;
 constexpr float kRescaleStep = 8.f;
 
 // shared-memory layout (offsets from a 1024-byte aligned base)
-constexpr uint32_t kOffQ = 0;                          // two query buffers
+constexpr uint32_t kOffQ = 0;                          // query rows of the two M-tiles
 constexpr uint32_t kOffK = kOffQ + 2u * kTileBytes;
 constexpr uint32_t kOffV = kOffK + kKStages * kTileBytes;
 constexpr uint32_t kOffBar = kOffV + kVStages * kTileBytes;
 constexpr uint32_t kOffMisc = kOffBar + 32 * 8;        // tmem address, abort flag
-constexpr uint32_t kOffBad = kOffMisc + 16;            // [8 tiles][8 blocks]: the block's values have no scale
-constexpr uint32_t kOffMark = kOffBad + 64;            // [half][warp]: rows that saw such a block
-constexpr uint32_t kOffXchg = kOffMark + 32;           // fp32 [half][row]
-constexpr uint32_t kSmemUsed = kOffXchg + 2 * 128 * 4;
+// [8 tiles][8 blocks]: the keys' scale, the exponent that the probabilities carry for the values, 2^-(that), and whether
+// the values have no scale (four fp32)
+constexpr uint32_t kOffMeta = kOffMisc + 16;
+constexpr uint32_t kSmemUsed = kOffMeta + 8 * 8 * 16;
 constexpr uint32_t kSmemBytes = kSmemUsed + 1024;      // slack to align the base
 static_assert(kSmemBytes <= 232448, "shared memory budget of one sm_100 block exceeded");
 
 enum Bar : int {
     kBarKFull = 0,   // [kKStages] converters -> MMA (one arrival per warp)
-    kBarKEmpty = 3,  // [kKStages] MMA (commit of the score product) -> converters
+    kBarKEmpty = 3,  // [kKStages] MMA (commit of the tile's last score product) -> converters
     kBarVFull = 6,   // [kVStages]
-    kBarVEmpty = 8,  // [kVStages]
-    kBarSFull = 10,  // [kSBufs] MMA (commit) -> softmax
-    kBarSFree = 13,  // [kSBufs] MMA (commit of P V) -> softmax: the accumulator holds the products up to this tile
-    kBarPReady = 16, // [kSBufs][2] softmax -> MMA: a warpgroup's half of the probabilities (4 arrivals)
-    kBarQReady = 20, // [2] softmax -> MMA: a unit's query rows are in their buffer (8 arrivals)
-    kBarDrain = 24,  // MMA (commit) -> MMA, on the way out
+    kBarVEmpty = 8,  // [kVStages] MMA (commit of the tile's last P V product) -> converters
+    kBarSFull = 10,  // [M-tile] MMA (commit, and an arrival that passes the converters' scales on) -> softmax: the scores are
+                     // there, and so is P V of the tile before
+    kBarPReady = 12, // [M-tile] softmax -> MMA (4 arrivals: one per warp)
+    kBarQReady = 14, // [M-tile] softmax -> MMA: a chain's query rows are in place (4 arrivals)
+    kBarOFull = 16,  // [M-tile] MMA (commit of P V) -> softmax
+    kBarDrain = 18,  // MMA (commit) -> MMA, on the way out
 };
 
-// Instruction descriptor: fp32 accumulator, bf16 A and B, both K-major, M = 128, N = 128.
-constexpr uint32_t kIdesc = umma_idesc_bf16(128u, 128u, false, false);
+// Instruction descriptors: fp32 accumulator, both operands K-major, M = 128, N = 128; fp16 (S) or bf16 (P V).
+constexpr uint32_t kIdescPV = umma_idesc_bf16(128u, 128u, false, false);
+constexpr uint32_t kIdescS = kIdescPV & ~((1u << 7) | (1u << 10));
 
-__device__ __forceinline__ void softmax_bar_both()
+// The eight instructions of a product (16 dims or tokens each; the operands' descriptors differ in their start address
+// only: 32 bytes per step, the second 64-element block kBlock on), issued by one thread.  D = A B, or with `accumulate`
+// D += A B.
+static_assert(kBlock == 16384u, "the steps' offsets below");
+__device__ __forceinline__ void product_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc)
 {
-    asm volatile("bar.sync 3, %0;" ::"n"(2 * kSoftmaxThreads) : "memory");
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        ".reg .b64 a, b;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "add.s64 a, %1, 0;\n"
+        "add.s64 b, %2, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
+        "setp.eq.b32 p, 0, 0;\n"
+        "add.s64 a, %1, 2;\n"
+        "add.s64 b, %2, 2;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
+        "add.s64 a, %1, 4;\n"
+        "add.s64 b, %2, 4;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
+        "add.s64 a, %1, 6;\n"
+        "add.s64 b, %2, 6;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
+        "add.s64 a, %1, 1024;\n"
+        "add.s64 b, %2, 1024;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
+        "add.s64 a, %1, 1026;\n"
+        "add.s64 b, %2, 1026;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
+        "add.s64 a, %1, 1028;\n"
+        "add.s64 b, %2, 1028;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
+        "add.s64 a, %1, 1030;\n"
+        "add.s64 b, %2, 1030;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
+        "}\n"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(kIdescS), "r"(0u)
+        : "memory");
+}
+__device__ __forceinline__ void product_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        ".reg .b64 a, b;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "add.s64 b, %2, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 0], b, %3, p;\n"
+        "setp.eq.b32 p, 0, 0;\n"
+        "add.s64 b, %2, 2;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 8], b, %3, p;\n"
+        "add.s64 b, %2, 4;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 16], b, %3, p;\n"
+        "add.s64 b, %2, 6;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 24], b, %3, p;\n"
+        "add.s64 b, %2, 1024;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 32], b, %3, p;\n"
+        "add.s64 b, %2, 1026;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 40], b, %3, p;\n"
+        "add.s64 b, %2, 1028;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 48], b, %3, p;\n"
+        "add.s64 b, %2, 1030;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 56], b, %3, p;\n"
+        "}\n"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(kIdescPV), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// pairs of fp32
+__device__ __forceinline__ uint64_t pair(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t a)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
 __device__ __forceinline__ uint32_t bf162_sub(uint32_t a, uint32_t b)
@@ -90,47 +203,43 @@ __device__ __forceinline__ uint32_t bf162_mul(uint32_t a, uint32_t b)
     return *reinterpret_cast<const uint32_t *>(&r);
 }
 
-// What multiplies a block's codes: one power of two (int8), or two (e4m3, whose bits are first read as bf16 numbers
-// 2^120 times too small), as pairs of bf16.
-struct Factor { uint32_t a, b; };
+// Four stored codes -> four fp16 numbers, exact (as in cart_q8.cu).
 template <int kFmt>
-__device__ __forceinline__ Factor factor_of(uint32_t eb)
+__device__ __forceinline__ uint2 to_f16(uint32_t r)
 {
-    Factor f;
+    uint2 o;
     if (kFmt == CART_Q8_INT8) {
-        f.a = eb == kQ8NoScale ? 0x7FC0u : eb << 7;
-        f.b = 0u;
+        const uint32_t a = __byte_perm(r, 0x64646464u, 0x4140), b = __byte_perm(r, 0x64646464u, 0x4342);
+        const __half2 off = __half2half2(__ushort_as_half((unsigned short)0x6480));
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), off), y = __hsub2(*reinterpret_cast<const __half2 *>(&b), off);
+        o.x = *reinterpret_cast<const uint32_t *>(&x);
+        o.y = *reinterpret_cast<const uint32_t *>(&y);
     } else {
-        // 2^120 2^e in two steps that bf16 holds: 2^100, and 2^(20 + e), -100 <= 20 + e <= 139: at most 2^127 for e <= 107;
-        // larger e (values beyond 2^107) give 2^7 of it to the first step
-        const uint32_t second = eb + 20u, over = second > 254u ? second - 254u : 0u;
-        f.a = eb == kQ8NoScale ? 0x7FC0u : (227u + over) << 7;
-        f.b = (second - over) << 7;
+        asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %2;\ncvt.rn.f16x2.e4m3x2 %0, l;\ncvt.rn.f16x2.e4m3x2 %1, h;\n}\n" : "=r"(o.x), "=r"(o.y) : "r"(r));
     }
-    f.a |= f.a << 16;
-    f.b |= f.b << 16;
-    return f;
+    return o;
 }
-// Four stored codes -> four bf16 values, exact.
+// Four stored codes -> four bf16 numbers, exact.
 template <int kFmt>
-__device__ __forceinline__ uint2 to_bf16(uint32_t r, const Factor f)
+__device__ __forceinline__ uint2 to_bf16(uint32_t r)
 {
     uint2 o;
     if (kFmt == CART_Q8_INT8) {
         // A byte u = code + 128 below the byte 0x43 reads, without its top bit, as the bf16 number 128 + (u mod 128); the
         // code is that less 128 if the top bit is set, less 256 if not.
         const uint32_t x = __byte_perm(r, 0x43434343u, 0x4140), y = __byte_perm(r, 0x43434343u, 0x4342);
-        o.x = bf162_mul(bf162_sub(x & 0xFF7FFF7Fu, (x & 0xFF80FF80u) ^ 0x00800080u), f.a);
-        o.y = bf162_mul(bf162_sub(y & 0xFF7FFF7Fu, (y & 0xFF80FF80u) ^ 0x00800080u), f.a);
+        o.x = bf162_sub(x & 0xFF7FFF7Fu, (x & 0xFF80FF80u) ^ 0x00800080u);
+        o.y = bf162_sub(y & 0xFF7FFF7Fu, (y & 0xFF80FF80u) ^ 0x00800080u);
     } else {
         // e4m3's exponent and mantissa bits, moved to the low end of bf16's exponent and the high end of its mantissa, are
         // the number times 2^-120, subnormals included.
         const uint32_t x = __byte_perm(r, 0u, 0x1404), y = __byte_perm(r, 0u, 0x3424);
-        o.x = bf162_mul(bf162_mul(((x >> 4) & 0x07F007F0u) | (x & 0x80008000u), f.a), f.b);
-        o.y = bf162_mul(bf162_mul(((y >> 4) & 0x07F007F0u) | (y & 0x80008000u), f.a), f.b);
+        o.x = bf162_mul(((x >> 4) & 0x07F007F0u) | (x & 0x80008000u), 0x7B807B80u);
+        o.y = bf162_mul(((y >> 4) & 0x07F007F0u) | (y & 0x80008000u), 0x7B807B80u);
     }
     return o;
 }
+constexpr int kFoldExp = 60;  // scales of values up to 2^+-60 are folded into the probabilities
 
 template <int kFmt>
 __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileParams p)
@@ -142,14 +251,13 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
     auto bar = [&](int i) { return base + kOffBar + (uint32_t)i * 8u; };
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + kOffMisc);
     volatile uint32_t *abort_flag = tmem_slot + 1;
-    volatile uint8_t *bad = smem + kOffBad;
-    volatile uint32_t *mark = reinterpret_cast<volatile uint32_t *>(smem + kOffMark);
 
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
     pdl_launch_dependents();
     const uint32_t unit_begin = p.unit_cta_begin[blockIdx.x];
     const uint32_t unit_end = p.unit_cta_begin[blockIdx.x + 1];
+    const uint32_t tpt = 128u / (uint32_t)p.group;   // readers per M-tile
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kKStages; ++i) {
@@ -160,493 +268,555 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
             mbar_init(bar(kBarVFull + i), kConvWarps);
             mbar_init(bar(kBarVEmpty + i), 1);
         }
-        for (int i = 0; i < kSBufs; ++i) {
-            mbar_init(bar(kBarSFull + i), 1);
-            mbar_init(bar(kBarSFree + i), 1);
-            mbar_init(bar(kBarPReady + 2 * i), 4);
-            mbar_init(bar(kBarPReady + 2 * i + 1), 4);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(kBarSFull + i), 2);
+            mbar_init(bar(kBarPReady + i), 4);
+            mbar_init(bar(kBarQReady + i), 4);
+            mbar_init(bar(kBarOFull + i), 1);
         }
-        for (int i = 0; i < 2; ++i) mbar_init(bar(kBarQReady + i), 8);
         mbar_init(bar(kBarDrain), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) {
+    if (warp == 0) {
+        __syncwarp();
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + kOffMisc), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = 0u;   // (all 512 columns are this block's: they begin at column 0)
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUtility));
-        if (warp == 1) {
-            // ================= MMA issuer: all lanes walk the loop and wait together, lane 0 issues ==========
-            const uint32_t issue = lane == 0 ? 1u : 0u;
+        if (warp == 0 && lane == 0) {
+            // ================= MMA issuer: one thread ========================================================
             bool ok = true;
-            auto wait_all = [&](int b, uint32_t parity) -> bool {
-                return __all_sync(0xffffffffu, mbar_wait(bar(b), parity, abort_flag, p.status, kStatusTimeoutMma));
+            auto wait = [&](int b, uint32_t parity) -> bool {
+                return mbar_wait(bar(b), parity, abort_flag, p.status, kStatusTimeoutMma);
             };
-            // Two cursors: `qk` names the next score product (two tiles ahead), `pv` the next P V product.
-            struct Cursor { uint32_t ui, t, n, unit_no, cont; };
-            auto tiles_of = [&](uint32_t ui) { return ui < unit_end ? p.units[ui].n_tiles : 0u; };
-            auto cont_of = [&](uint32_t ui) { return ui < unit_end ? (uint32_t)(p.units[ui].flags & CART_UNIT_CONT) : 0u; };
-            Cursor qk{unit_begin, 0u, tiles_of(unit_begin), 0u, cont_of(unit_begin)}, pv = qk;
-            auto advance = [&](Cursor &c) {
-                if (++c.t == c.n) {
-                    ++c.ui;
-                    c.t = 0;
-                    c.n = tiles_of(c.ui);
-                    c.cont = cont_of(c.ui);
-                    if (c.cont == 0u) ++c.unit_no;   // (a unit that continues a chain keeps its rows)
-                }
+            // where the next score products are: unit, tile in it, tiles of the unit; the chain before it
+            uint32_t ui = unit_begin, t = 0, n = 0, two = 0, fresh = 1;
+            auto unit = [&]() {
+                if (ui >= unit_end) return;
+                const cart_shared_unit u = p.units[ui];
+                n = u.n_tiles;
+                two = u.n_readers > tpt ? 1u : 0u;
+                fresh = (u.flags & CART_UNIT_CONT) ? 0u : 1u;
             };
-            uint32_t total = 0;
-            for (uint32_t ui = unit_begin; ui < unit_end; ++ui) total += p.units[ui].n_tiles;
-            // S(tt) = Q K^T into score buffer tt % 2, which tile tt - 2's P V products, issued earlier, read
-            auto issue_s = [&](uint32_t tt) -> bool {
-                const uint32_t sb = tt % (uint32_t)kSBufs;
-                const uint32_t kst = tt % (uint32_t)kKStages, kpar = (tt / (uint32_t)kKStages) & 1u;
-                const uint32_t qb = qk.unit_no & 1u;
-                if (qk.t == 0u && qk.cont == 0u && !wait_all(kBarQReady + (int)qb, (qk.unit_no >> 1) & 1u)) return false;
-                if (!wait_all(kBarKFull + (int)kst, kpar)) return false;
+            unit();
+            uint32_t q_uses[2] = {0u, 0u};   // chains whose rows M-tile x has taken
+            uint32_t p_uses[2] = {0u, 0u};   // tiles whose probabilities M-tile x has delivered
+            uint32_t kst = 0, kpar = 0, vst = 0, vpar = 0;
+            // S_x = Q_x K^T: S_x last held probabilities, which P V products issued earlier by this thread read
+            auto issue_s = [&](uint32_t x) {
                 tc_fence_after();
-                const uint64_t a0 = umma_desc(base + kOffQ + qb * kTileBytes, 16, 1024);
-                const uint64_t b0 = umma_desc(base + kOffK + kst * kTileBytes, 16, 1024);
-                const uint32_t d_s = tmem + sb * 128u;
-#pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) {  // 16 dims per instruction
-                    const uint64_t off16 = (uint64_t)(((k >> 2) * kBlock + (k & 3u) * 32u) >> 4);
-                    umma_bf16(d_s, a0 + off16, b0 + off16, kIdesc, k, issue);
-                }
-                umma_commit(bar(kBarSFull + (int)sb), issue);
-                umma_commit(bar(kBarKEmpty + (int)kst), issue);
-                advance(qk);
+                product_ss(tmem + x * 128u, umma_desc(base + kOffQ + x * kTileBytes, 16, 1024), umma_desc(base + kOffK + kst * kTileBytes, 16, 1024));
+                mma_commit(bar(kBarSFull + (int)x));
+                mbar_arrive(bar(kBarSFull + (int)x));
+            };
+            // O_x += P_x V (O_x = P_x V for a chain's first tile)
+            auto issue_pv = [&](uint32_t x, uint32_t first) {
+                tc_fence_after();
+                product_ts(tmem + kTmemO + 128u * x, tmem + x * 128u, umma_desc(base + kOffV + vst * kTileBytes, 16, 1024), first ? 0u : 1u);
+                mma_commit(bar(kBarOFull + (int)x));
+            };
+            // the next tile's scores for M-tile x, if there is one (its rows first, where a chain begins)
+            auto next_s = [&](uint32_t x, bool k_wait) -> bool {
+                if (fresh && t == 0u && !wait(kBarQReady + (int)x, q_uses[x]++ & 1u)) return false;
+                if (k_wait && !wait(kBarKFull + (int)kst, kpar)) return false;
+                issue_s(x);
                 return true;
             };
-            // O_x += P_x V_x for both halves x of the tile's tokens; V's half x is the swizzled block x: rows are dims
-            auto issue_pv = [&](uint32_t tt) -> bool {
-                const uint32_t sb = tt % (uint32_t)kSBufs, spar = (tt / (uint32_t)kSBufs) & 1u;
-                const uint32_t vst = tt % (uint32_t)kVStages, vpar = (tt / (uint32_t)kVStages) & 1u;
-                if (!wait_all(kBarVFull + (int)vst, vpar)) return false;
-                const uint64_t b0 = umma_desc(base + kOffV + vst * kTileBytes, 16, 1024);
-                const uint32_t p_tm = tmem + sb * 128u;
-                const uint32_t d_o = tmem + kTmemO;
-                const bool first = pv.t == 0u && pv.cont == 0u;  // (a unit that continues a chain adds to its accumulators)
-#pragma unroll
-                for (uint32_t x = 0; x < 2; ++x) {
-                    if (!wait_all(kBarPReady + 2 * (int)sb + (int)x, spar)) return false;
-                    tc_fence_after();
-#pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k)  // 16 tokens per instruction
-                        umma_bf16_ts(d_o + 128u * x, p_tm + 64u * x + 8u * k, b0 + (uint64_t)((x * kBlock + k * 32u) >> 4), kIdesc,
-                                     (first && k == 0u) ? 0u : 1u, issue);
+            auto next_tile = [&]() {
+                mma_commit(bar(kBarKEmpty + (int)kst));
+                if (++kst == (uint32_t)kKStages) {
+                    kst = 0;
+                    kpar ^= 1u;
                 }
-                umma_commit(bar(kBarVEmpty + (int)vst), issue);
-                umma_commit(bar(kBarSFree + (int)sb), issue);
-                advance(pv);
-                return true;
+                if (++t == n) {
+                    ++ui;
+                    t = 0;
+                    unit();
+                }
             };
-            if (total > 0u) ok = issue_s(0u);
-            if (ok && total > 1u) ok = issue_s(1u);
-            for (uint32_t tt = 0; tt < total && ok; ++tt) {
-                ok = issue_pv(tt);
-                if (ok && tt + 2u < total) ok = issue_s(tt + 2u);
+            // the tile in front: how many M-tiles it has, whether it begins a chain
+            uint32_t cur_two = two, cur_first = fresh;
+            if (ui < unit_end) {
+                ok = next_s(0u, true);
+                if (ok && two) ok = next_s(1u, false);
+                if (ok) next_tile();
+                while (ok) {
+                    const bool more = ui < unit_end;
+                    const uint32_t nxt_two = two, nxt_first = (t == 0u && fresh) ? 1u : 0u;
+                    ok = wait(kBarVFull + (int)vst, vpar) && wait(kBarPReady, p_uses[0]++ & 1u);
+                    if (!ok) break;
+                    issue_pv(0u, cur_first);
+                    if (more) {
+                        ok = next_s(0u, true);
+                        if (!ok) break;
+                    }
+                    if (cur_two) {
+                        ok = wait(kBarPReady + 1, p_uses[1]++ & 1u);
+                        if (!ok) break;
+                        issue_pv(1u, cur_first);
+                    }
+                    mma_commit(bar(kBarVEmpty + (int)vst));
+                    if (++vst == (uint32_t)kVStages) {
+                        vst = 0;
+                        vpar ^= 1u;
+                    }
+                    if (!more) break;
+                    if (nxt_two) {
+                        ok = next_s(1u, false);
+                        if (!ok) break;
+                    }
+                    next_tile();
+                    cur_two = nxt_two;
+                    cur_first = nxt_first;
+                }
             }
             // products still in flight must finish before the tensor memory is given back
-            umma_commit(bar(kBarDrain), issue);
+            mma_commit(bar(kBarDrain));
             const uint64_t t0 = global_timer_ns();
             while (!mbar_try_wait(bar(kBarDrain), 0) && global_timer_ns() - t0 < kWaitLimitNs) {}
-            __syncwarp();
         }
     } else if (warp >= 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
         // ================= converters: codes -> bf16 operand tiles ======================================
-        // Warp w takes the blocks w and w + 4 of every tile, first of the keys, then of the values: four tasks per tile.
-        const uint32_t cw = (uint32_t)warp - 12u;
+        // Warp w takes the blocks w and w + 4 of every tile (block w of either page), their keys and then their values.
+        const uint32_t b = (uint32_t)warp - 12u;
         const uint32_t g = (uint32_t)lane >> 2, t4 = (uint32_t)lane & 3u;
-        uint32_t total = 0;
-        for (uint32_t ui = unit_begin; ui < unit_end; ++ui) total += p.units[ui].n_tiles;
         pdl_wait();  // the codes may come from the kernel before
-        // the loading side runs one task ahead: where its tile lies
-        uint32_t l_ui = unit_begin, l_t = 0, l_row = 0, l_head = 0, l_tiles = 0, l_tok = 0;
-        auto l_unit = [&]() {
-            if (l_ui >= unit_end) return;
-            const cart_shared_unit u = p.units[l_ui];
-            l_row = u.k_row;
-            l_head = (uint32_t)p.layer * u.layer_stride + u.v_row;
-            l_tiles = u.n_tiles;
-            l_tok = (u.flags & CART_UNIT_MASKED) ? (uint32_t)(u.lim_cap + 1) : u.n_tiles * (uint32_t)kTile;
+        // where the tile whose codes are requested next lies
+        uint32_t ui = unit_begin, t = 0, n = 0, row = 0, tok_end = 0;
+        uint32_t page[2] = {0u, 0u}, page_next[2] = {0u, 0u};   // base rows of its two pages, and of the next tile's
+        const uint8_t *head = nullptr;   // the warp's block of the KV head, in a page at row 0
+        auto page_of = [&](uint32_t tile, uint32_t y) {   // (the list may end before the last tile's second page)
+            return tile < n && tile * (uint32_t)kTile + y * 64u < tok_end ? __ldg(p.pages + row + 2u * tile + y) : 0u;
         };
-        l_unit();
-        uint32_t pg[2] = {0u, 0u};       // base rows of the two pages of the tile being loaded
-        auto l_pages = [&]() {
-            if (l_ui >= unit_end) return;
-            pg[0] = __ldg(p.pages + l_row + 2u * l_t);
-            pg[1] = l_t * (uint32_t)kTile + 64u < l_tok ? __ldg(p.pages + l_row + 2u * l_t + 1u) : 0u;
-        };
-        l_pages();
-        struct Task { uint4 x[4]; uint32_t scales, left; };  // left: tokens of the block that exist (may exceed 16)
-        auto load = [&](Task &k, uint32_t half, bool values) {
-            const uint32_t b = cw + 4u * half, tok = l_t * (uint32_t)kTile + b * 16u;
-            k.left = l_ui < unit_end && tok < l_tok ? l_tok - tok : 0u;
-            k.scales = 0u;
-            if (k.left == 0u) return;
-            const uint8_t *blk = p.arena + (size_t)pg[half] * kRowBytes + ((size_t)l_head * (kTileTokens / kQ8Block) + cw) * kQ8BlockBytes;
-            const uint4 *src = reinterpret_cast<const uint4 *>(blk + (values ? kQ8ValueOff : 0u)) + lane;
+        auto unit = [&]() {
+            if (ui >= unit_end) return;
+            const cart_shared_unit u = p.units[ui];
+            row = u.k_row;
+            head = p.arena + ((size_t)((uint32_t)p.layer * u.layer_stride + u.v_row) * (kTileTokens / kQ8Block) + b) * kQ8BlockBytes;
+            n = u.n_tiles;
+            tok_end = (u.flags & CART_UNIT_MASKED) ? (uint32_t)(u.lim_cap + 1) : u.n_tiles * (uint32_t)kTile;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) k.x[c] = src[32 * c];
-            k.scales = *reinterpret_cast<const uint16_t *>(blk + kQ8ScaleOff);
+            for (uint32_t y = 0; y < 2; ++y) {
+                page[y] = page_of(0u, y);
+                page_next[y] = page_of(1u, y);
+            }
         };
-        Task k0, k1;  // two tasks in flight
-        if (total > 0u) {
-            load(k0, 0u, false);
-            load(k1, 1u, false);
-        }
-        bool ok = true;
-        auto wait_conv = [&](int b, uint32_t parity) -> bool {
-            return __all_sync(0xffffffffu, mbar_wait(bar(b), parity, abort_flag, p.status, kStatusTimeoutProducer));
+        unit();
+        struct Codes { uint4 x[4]; };
+        // of the tile whose keys were requested last: scale bytes; tokens of the block that exist (may exceed 16)
+        uint32_t scales[2] = {0u, 0u}, left[2] = {0u, 0u};
+        const uint8_t *blk[2] = {nullptr, nullptr};
+        auto load = [&](Codes &k, const uint8_t *at) {
+            const uint4 *src = reinterpret_cast<const uint4 *>(at) + lane;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) k.x[c] = __ldcg(src + 32 * c);
         };
-        auto put_keys = [&](const Task &k, uint32_t b, uint32_t dst, uint32_t tt) {
-            if (lane == 0) bad[(tt & 7u) * 8u + b] = k.left > 0u && (k.scales >> 8) == kQ8NoScale ? 1 : 0;
-            if (k.left == 0u) return;  // (scores of keys that do not exist are masked, whatever stands there)
-            const Factor f = factor_of<kFmt>(k.scales & 0xFFu);
+        // requests the keys of the next tile; false: there is none
+        auto next_keys = [&](Codes (&k)[2]) -> bool {
+            if (ui >= unit_end) return false;
 #pragma unroll
-            for (uint32_t c = 0; c < 4; ++c) {
-                const uint32_t w[4] = {k.x[c].x, k.x[c].y, k.x[c].z, k.x[c].w};
-#pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) {
-                    const uint32_t ks = 2u * c + (j >> 1), row = 16u * b + g + 8u * (j & 1u);
-                    const uint2 v = to_bf16<kFmt>(w[j], f);
-                    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(dst + (ks >> 2) * kBlock + row * 128u +
-                                                                         (((2u * (ks & 3u) + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u),
-                                 "r"(v.x), "r"(v.y)
-                                 : "memory");
+            for (uint32_t y = 0; y < 2; ++y) {
+                const uint32_t tok = t * (uint32_t)kTile + y * 64u + b * 16u;
+                left[y] = tok < tok_end ? tok_end - tok : 0u;
+                scales[y] = 0u;
+                if (left[y] > 0u) {
+                    blk[y] = head + (size_t)page[y] * kRowBytes;
+                    load(k[y], blk[y]);
+                    scales[y] = __ldcg(reinterpret_cast<const unsigned short *>(blk[y] + kQ8ScaleOff));
                 }
+                page[y] = page_next[y];
             }
+            if (++t == n) {
+                ++ui;
+                t = 0;
+                unit();
+            } else {
+                page_next[0] = page_of(t + 1u, 0u);
+                page_next[1] = page_of(t + 1u, 1u);
+            }
+            return true;
         };
-        auto put_values = [&](const Task &k, uint32_t b, uint32_t dst) {
-            const uint32_t eb = k.scales >> 8;
-            const bool none = k.left == 0u || eb == kQ8NoScale;
-            const Factor f = factor_of<kFmt>(none ? 127u : eb);
-            uint32_t m0 = 0xFFFFFFFFu, m1 = 0xFFFFFFFFu;   // tokens behind the end count as zeros
-            if (none) {
-                m0 = m1 = 0u;
-            } else if (k.left < 16u) {
-                m0 = (2u * t4 < k.left ? 0xFFFFu : 0u) | (2u * t4 + 1u < k.left ? 0xFFFF0000u : 0u);
-                m1 = (2u * t4 + 8u < k.left ? 0xFFFFu : 0u) | (2u * t4 + 9u < k.left ? 0xFFFF0000u : 0u);
-            }
-#pragma unroll
-            for (uint32_t c = 0; c < 4; ++c) {
-                const uint32_t w[4] = {k.x[c].x, k.x[c].y, k.x[c].z, k.x[c].w};
-#pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) {
-                    const uint32_t dim = 16u * (2u * c + (j >> 1)) + g + 8u * (j & 1u);
-                    const uint2 v = to_bf16<kFmt>(w[j], f);
-                    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(dst + (b >> 2) * kBlock + dim * 128u +
-                                                                         (((2u * (b & 3u) + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u),
-                                 "r"(v.x & m0), "r"(v.y & m1)
-                                 : "memory");
-                }
-            }
+        Codes ck[2], cv[2];
+        bool ok = true, more = next_keys(ck);
+        uint32_t kst = 0, kpar = 1, vst = 0, vpar = 1, tt = 0;
+        auto wait_conv = [&](int x, uint32_t parity) -> bool {
+            return __all_sync(0xffffffffu, mbar_wait(bar(x), parity, abort_flag, p.status, kStatusTimeoutProducer));
         };
-        for (uint32_t tt = 0; tt < total && ok; ++tt) {
-            const uint32_t kst = tt % (uint32_t)kKStages, kpar = (tt / (uint32_t)kKStages) & 1u;
-            const uint32_t vst = tt % (uint32_t)kVStages, vpar = (tt / (uint32_t)kVStages) & 1u;
-            ok = wait_conv(kBarKEmpty + (int)kst, kpar ^ 1u);
+        // 8-byte stores: word (c, j) of a lane goes to row 64 y + 16 b + g + 8 (j & 1) [keys], dims 16 (2 c + j / 2) + 4 t4 ..;
+        // or [values] to dim 16 (2 c + j / 2) + g + 8 (j & 1), stored tokens 64 y + 16 b + 4 t4 ..
+        const uint32_t k_at = (16u * b + g) * 128u + (t4 & 1u) * 8u;
+        const uint32_t v_at = g * 128u + (((2u * b + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u;
+        while (more) {
+            uint32_t cur_scales[2], cur_left[2];
+#pragma unroll
+            for (uint32_t y = 0; y < 2; ++y) {
+                cur_scales[y] = scales[y];
+                cur_left[y] = left[y];
+                if (cur_left[y] > 0u) load(cv[y], blk[y] + kQ8ValueOff);
+            }
+            ok = wait_conv(kBarKEmpty + (int)kst, kpar);
             if (!ok) break;
-            put_keys(k0, cw, base + kOffK + kst * kTileBytes, tt);
-            load(k0, 0u, true);
-            put_keys(k1, cw + 4u, base + kOffK + kst * kTileBytes, tt);
-            load(k1, 1u, true);
+#pragma unroll
+            for (uint32_t y = 0; y < 2; ++y) {
+                if (lane == 0) {
+                    const uint32_t ek = cur_scales[y] & 0xFFu, ev = cur_scales[y] >> 8;
+                    const bool none = cur_left[y] == 0u || ev == kQ8NoScale;
+                    const int fold = none ? 0 : min(max((int)ev - 127, -kFoldExp), kFoldExp);
+                    // (a block without tokens: no scale is read, its scores are masked)
+                    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + kOffMeta + ((tt & 7u) * 8u + 4u * y + b) * 16u),
+                                 "f"(ek == kQ8NoScale ? __uint_as_float(0x7FC00000u) : __uint_as_float(ek << 23)), "f"((float)fold),
+                                 "f"(__uint_as_float((uint32_t)(127 - fold) << 23)), "f"(cur_left[y] > 0u && ev == kQ8NoScale ? 1.f : 0.f)
+                                 : "memory");
+                }
+                if (cur_left[y] == 0u) continue;   // (scores of keys that do not exist are masked, whatever stands there)
+                const uint32_t dst = base + kOffK + kst * kTileBytes + y * (kBlock / 2u) + k_at;
+#pragma unroll
+                for (uint32_t c = 0; c < 4; ++c) {
+                    const uint32_t w[4] = {ck[y].x[c].x, ck[y].x[c].y, ck[y].x[c].z, ck[y].x[c].w};
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) {
+                        const uint32_t ks = 2u * c + (j >> 1);
+                        const uint2 v = to_f16<kFmt>(w[j]);
+                        asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(dst + (ks >> 2) * kBlock + (j & 1u) * 1024u +
+                                                                             (((2u * (ks & 3u) + (t4 >> 1)) ^ g) << 4)),
+                                     "r"(v.x), "r"(v.y)
+                                     : "memory");
+                    }
+                }
+            }
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kBarKFull + (int)kst));
-            // the loading side goes on to the next tile
-            if (++l_t == l_tiles) {
-                ++l_ui;
-                l_t = 0;
-                l_unit();
+            if (++kst == (uint32_t)kKStages) {
+                kst = 0;
+                kpar ^= 1u;
             }
-            l_pages();
-            ok = wait_conv(kBarVEmpty + (int)vst, vpar ^ 1u);
+            more = next_keys(ck);
+            ok = wait_conv(kBarVEmpty + (int)vst, vpar);
             if (!ok) break;
-            put_values(k0, cw, base + kOffV + vst * kTileBytes);
-            load(k0, 0u, false);
-            put_values(k1, cw + 4u, base + kOffV + vst * kTileBytes);
-            load(k1, 1u, false);
+#pragma unroll
+            for (uint32_t y = 0; y < 2; ++y) {
+                const uint32_t eb = cur_scales[y] >> 8;
+                const bool none = cur_left[y] == 0u || eb == kQ8NoScale;
+                // (beyond what the probabilities carry)
+                const int over = none ? 0 : (int)eb - 127 - min(max((int)eb - 127, -kFoldExp), kFoldExp);
+                const uint32_t extra = (uint32_t)(127 + over) << 7, extra2 = extra | extra << 16;
+                uint32_t m0 = 0xFFFFFFFFu, m1 = 0xFFFFFFFFu;   // tokens behind the end count as zeros
+                if (none) {
+                    m0 = m1 = 0u;
+                } else if (cur_left[y] < 16u) {
+                    m0 = (2u * t4 < cur_left[y] ? 0xFFFFu : 0u) | (2u * t4 + 1u < cur_left[y] ? 0xFFFF0000u : 0u);
+                    m1 = (2u * t4 + 8u < cur_left[y] ? 0xFFFFu : 0u) | (2u * t4 + 9u < cur_left[y] ? 0xFFFF0000u : 0u);
+                }
+                const uint32_t dst = base + kOffV + vst * kTileBytes + y * kBlock + v_at;
+#pragma unroll
+                for (uint32_t c = 0; c < 4; ++c) {
+                    const uint32_t w[4] = {cv[y].x[c].x, cv[y].x[c].y, cv[y].x[c].z, cv[y].x[c].w};
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) {
+                        uint2 v = to_bf16<kFmt>(w[j]);
+                        if (over != 0) {
+                            v.x = bf162_mul(v.x, extra2);
+                            v.y = bf162_mul(v.y, extra2);
+                        }
+                        asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(dst + (2u * c + (j >> 1)) * 2048u + (j & 1u) * 1024u),
+                                     "r"(v.x & m0), "r"(v.y & m1)
+                                     : "memory");
+                    }
+                }
+            }
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kBarVFull + (int)vst));
+            if (++vst == (uint32_t)kVStages) {
+                vst = 0;
+                vpar ^= 1u;
+            }
+            ++tt;
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-        // ================= softmax / epilogue warps ====================================================
-        const int G = p.group;
-        const int wg = (warp - 4) >> 2;       // which 64 score columns (tokens) of every tile this thread owns
-        const int sw = warp & 3;              // the tensor-memory lanes this warp may read: 32 sw .. 32 sw + 31
-        const int row = 32 * sw + lane;       // query row of the M-tile = tensor-memory lane
-        const uint32_t lane_addr = tmem + ((uint32_t)(32 * sw) << 16);
-        const uint32_t col0 = 64u * (uint32_t)wg;
-        float *xchg = reinterpret_cast<float *>(smem + kOffXchg);           // [half][row]
-        uint32_t tt = 0;      // tiles of the block so far
-        bool alive = true;    // false once the block has given up: work is skipped, barriers are still met
-        auto warp_wait = [&](uint32_t b, uint32_t parity) -> bool {
-            return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag, p.status, kStatusTimeoutConsumer));
+        // ================= softmax / epilogue warps: warpgroup x has M-tile x, a thread has a row ============
+        const uint32_t G = (uint32_t)p.group;
+        const uint32_t x = (uint32_t)(warp - 4) >> 2;
+        const uint32_t sw = (uint32_t)warp & 3u;             // the tensor-memory lanes this warp may read: 32 sw ..
+        const uint32_t row = 32u * sw + (uint32_t)lane;
+        const uint32_t lane_addr = tmem + ((32u * sw) << 16);
+        const uint32_t s_addr = lane_addr + 128u * x, o_addr = lane_addr + kTmemO + 128u * x;
+        const uint32_t i_row = row / G, h = row - i_row * G;
+        const uint32_t i_reader = i_row < tpt ? i_row + x * tpt : 0xFFFFFFu;   // (128 may not be a multiple of G)
+        bool alive = true;    // false once the block has given up: work is skipped
+        auto warp_wait = [&](int b, uint32_t parity) -> bool {
+            return __all_sync(0xffffffffu, mbar_wait(bar(b), parity, abort_flag, p.status, kStatusTimeoutConsumer));
         };
-        const uint32_t o_addr = lane_addr + kTmemO + 128u * (uint32_t)wg;   // this warpgroup's accumulator: 128 columns
-
-        // Query rows: thread (w, r) copies the 64-dim half w of row r into the unit's query buffer, in the swizzled K-major
-        // operand layout; rows past the unit's readers are zeros.  (As in cart_shared.cu.)
-        const int i_reader = row / G, h = row - i_reader * G;
-        const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(p.q);
-        auto load_q = [&](uint32_t kv_head, uint32_t batch, bool on, uint32_t buf) {
-            const uint8_t *src = reinterpret_cast<const uint8_t *>(q + ((size_t)batch * p.n_q_heads + (size_t)kv_head * G + h) * kHeadDim) + 128 * wg;
-            const uint32_t qrow = base + kOffQ + buf * kTileBytes + (uint32_t)wg * kBlock + (uint32_t)row * 128u;
-            const uint32_t swz = (uint32_t)(row & 7);
+        // The row into the swizzled K-major operand -- block w (64 dims), 16-byte chunk c at position c ^ (row % 8) -- as fp16
+        // over the power of two that brings its largest value to 1 .. 2 (see cart_q8.cu); a row with a NaN or an infinity
+        // as NaN, rows past the readers as zeros.  Returns what takes its scores to base-2 exponents: 2^e scale log2(e).
+        const uint32_t q_row = base + kOffQ + x * kTileBytes + row * 128u;
+        auto q_src = [&](uint32_t kv_head, uint32_t batch) {
+            return reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) +
+                                                   ((size_t)batch * p.n_q_heads + (size_t)kv_head * G + h) * kHeadDim);
+        };
+        auto bring_q = [&](uint32_t kv_head, uint32_t batch, bool on) -> float {
+            const uint4 *src = q_src(kv_head, batch);
+            uint32_t big = 0u;
+            if (on) {
+#pragma unroll 8
+                for (uint32_t c = 0; c < 16; ++c) {
+                    const uint4 v = __ldg(src + c);
+                    big = __vmaxu2(big, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
+                }
+                big = max(big & 0xFFFFu, big >> 16);
+            }
+            const int qe = big >= 0x7F80u ? 0 : min(max((int)(big >> 7), 2) - 127, 126);
+            const float down = big >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - qe) << 23);
+#pragma unroll 4
+            for (uint32_t c = 0; c < 16; ++c) {
+                uint32_t w[4] = {0u, 0u, 0u, 0u};
+                if (on) {
+                    const uint4 v = __ldg(src + c);
+                    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (uint32_t c = 0; c < 8; ++c)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(qrow + ((c ^ swz) << 4)),
-                             "l"(on ? src + 16u * c : reinterpret_cast<const uint8_t *>(q)), "r"(on ? 16u : 0u)
+                    for (int j = 0; j < 4; ++j) {
+                        const __half2 y = __floats2half2_rn(__uint_as_float(r[j] << 16) * down, __uint_as_float(r[j] & 0xFFFF0000u) * down);
+                        w[j] = *reinterpret_cast<const uint32_t *>(&y);
+                    }
+                }
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_row + (c >> 3) * kBlock + (((c & 7u) ^ (row & 7u)) << 4)), "r"(w[0]),
+                             "r"(w[1]), "r"(w[2]), "r"(w[3])
                              : "memory");
-        };
-        // Waits for the copies, tells the MMA warp; true if this thread's half of the row holds a NaN or an infinity.
-        auto store_q = [&](uint32_t buf) -> bool {
-            asm volatile("cp.async.wait_all;" ::: "memory");
+            }
             fence_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kBarQReady + (int)buf));
-            const uint32_t qrow = base + kOffQ + buf * kTileBytes + (uint32_t)wg * kBlock + (uint32_t)row * 128u;
-            uint32_t big = 0u;
-#pragma unroll
-            for (uint32_t c = 0; c < 8; ++c) {
-                uint32_t a0, a1, a2, a3;
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3) : "r"(qrow + 16u * c));
-                big = __vmaxu2(big, __vmaxu2(__vmaxu2(a0 & 0x7FFF7FFFu, a1 & 0x7FFF7FFFu), __vmaxu2(a2 & 0x7FFF7FFFu, a3 & 0x7FFF7FFFu)));
-            }
-            return (big & 0xFFFFu) >= 0x7F80u || (big >> 16) >= 0x7F80u;
+            if (lane == 0) mbar_arrive(bar(kBarQReady + (int)x));
+            return __uint_as_float((uint32_t)(qe + 127) << 23) * p.scale_log2;
         };
-        cart_shared_unit u{}, u_next{};
-        bool q_bad = false, q_bad_next = false;
-        pdl_wait();  // q, the partial slots and out belong to the kernels before until they are done
-        if (unit_begin < unit_end) {
-            u = p.units[unit_begin];
-            const bool on = (uint32_t)i_reader < u.n_readers;
-            load_q(u.kv_head, on ? p.readers[u.reader_begin + (uint32_t)i_reader] : 0u, on, 0u);
-            if (unit_begin + 1u < unit_end) u_next = p.units[unit_begin + 1u];
-            q_bad_next = store_q(0u);
-        }
-
+        auto has_rows = [&](const cart_shared_unit &u) { return x == 0u || u.n_readers > tpt; };   // the M-tile takes part
+        uint32_t uses = 0;       // tiles of this M-tile so far
+        uint32_t tiles = 0;      // tiles of the block so far
         float m_run = -INFINITY, l_run = 0.f;
-        bool fresh = true;      // no tile of the chain has been seen yet
-        bool marked = false;    // the row has seen values without a scale
-        uint32_t unit_no = 0;   // counts the units that bring their own query rows
+        bool fresh = true;       // no tile of the chain has been seen yet
+        bool marked = false;     // the row has seen values without a scale
+        float f_row = 0.f, f_next = 0.f;   // see bring_q: of this chain's rows, of the next one's
+        uint32_t uq_next = unit_begin;   // the unit whose rows are fetched next (a chain's first that this M-tile takes part in)
+        auto first_chain = [&](uint32_t from) {   // from: a chain's first unit
+            while (from < unit_end && !has_rows(p.units[from])) from += p.units[from].reserved;
+            return from;
+        };
+        pdl_wait();  // q, the partial slots and out belong to the kernels before until they are done
+        uq_next = first_chain(unit_begin);
+        if (uq_next < unit_end) {
+            const cart_shared_unit u = p.units[uq_next];
+            const bool on = i_reader < u.n_readers;
+            f_next = bring_q(u.kv_head, on ? p.readers[u.reader_begin + i_reader] : 0u, on);
+        }
+        cart_shared_unit u{}, u_next{};
+        if (unit_begin < unit_end) u_next = p.units[unit_begin];
+        uint32_t batch_next = 0, head_next = 0;
+        bool on_next = false;
         for (uint32_t ui = unit_begin; ui < unit_end; ++ui) {
-            if (ui != unit_begin) {
-                u = u_next;
-                u_next = cart_shared_unit{};
-                if (ui + 1u < unit_end) u_next = p.units[ui + 1u];
+            u = u_next;
+            if (ui + 1u < unit_end) u_next = p.units[ui + 1u];
+            if (!has_rows(u)) {
+                tiles += u.n_tiles;
+                continue;
             }
-            const bool brings_rows = !(u.flags & CART_UNIT_CONT);
-            if (brings_rows && ui != unit_begin) ++unit_no;
-            // the next unit with rows of its own (`reserved` says how many units on it comes: 0, the next one of another
-            // chain is not in this block)
-            bool has_next = false;
-            cart_shared_unit uq{};
-            if (brings_rows) {
-                const uint32_t uj = ui + (u.reserved ? u.reserved : (unit_end - ui));
-                has_next = uj < unit_end;
-                if (has_next) uq = uj == ui + 1u ? u_next : p.units[uj];
-                q_bad = q_bad_next;
-                q_bad_next = false;
-                m_run = -INFINITY;
-                // (a query with a NaN or an infinity in it: all of its row becomes NaN)
-                l_run = q_bad ? __uint_as_float(0x7FC00000u) : 0.f;
-                fresh = true;
-                marked = false;
-            }
-            const bool valid = (uint32_t)i_reader < u.n_readers;
-            // The next rows are requested in steps a tile apart, so that nobody waits for the reads they hang on.
-            const uint32_t last = u.n_tiles - 1u;
-            const uint32_t t_reader = last < 1u ? last : 1u, t_load = last < 2u ? last : 2u, t_store = last < 4u ? last : 4u;
-            bool valid_next = false;
-            uint32_t batch_next = 0;
+            const bool valid = i_reader < u.n_readers;
             const bool direct = (u.flags & CART_UNIT_DIRECT) != 0u, hold = (u.flags & CART_UNIT_HOLD) != 0u;
             const bool masked = (u.flags & CART_UNIT_MASKED) != 0u;
-            uint32_t slot = 0;   // where this row's partial goes, or (direct) its query row: needed at the unit's end
+            if (!(u.flags & CART_UNIT_CONT)) {
+                m_run = -INFINITY;
+                l_run = 0.f;
+                f_row = f_next;
+                fresh = true;
+                marked = false;
+                // the next chain's rows: what the copy hangs on is read now, long before its last tile
+                uq_next = first_chain(ui + u.reserved);
+                on_next = false;
+                if (uq_next < unit_end) {
+                    const cart_shared_unit uq = p.units[uq_next];
+                    on_next = i_reader < uq.n_readers;
+                    head_next = uq.kv_head;
+                    batch_next = on_next ? p.readers[uq.reader_begin + i_reader] : 0u;
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(q_src(head_next, batch_next)));
+                }
+            }
+            uint32_t slot = 0;   // where this row's partial goes, or (direct) its query row: needed at the chain's end
             if (valid && !hold)
-                slot = direct ? p.readers[u.reader_begin + (uint32_t)i_reader]
-                              : p.reader_slot[(size_t)(u.reader_begin + (uint32_t)i_reader) * p.n_kv_heads + u.kv_head] + u.chunk;
+                slot = direct ? p.readers[u.reader_begin + i_reader]
+                              : p.reader_slot[(size_t)(u.reader_begin + i_reader) * p.n_kv_heads + u.kv_head] + u.chunk;
             int32_t limit = 0x7FFFFFFF;   // masked run: the last key of the run this row sees (-1: none)
             if (masked) {
-                // (the run belongs to the readers tr_hi >> 16 .. (tr_hi & 0xFFFF) - 1 of the M-tile)
-                const int32_t lb = u.lim_base + i_reader;
-                const bool in = (uint32_t)i_reader < (u.tr_hi & 0xFFFFu) && (uint32_t)i_reader >= u.tr_hi >> 16;
+                // (the run belongs to the readers tr_hi >> 16 .. (tr_hi & 0xFFFF) - 1 of the unit)
+                const int32_t lb = u.lim_base + (int32_t)i_reader;
+                const bool in = i_reader < (u.tr_hi & 0xFFFFu) && i_reader >= u.tr_hi >> 16;
                 limit = in && lb >= 0 ? (lb < u.lim_cap ? lb : u.lim_cap) : -1;
             }
-
-            for (uint32_t t = 0; t < u.n_tiles; ++t, ++tt) {
-                const uint32_t sb = tt % (uint32_t)kSBufs, spar = (tt / (uint32_t)kSBufs) & 1u;
-                const uint32_t s_addr = lane_addr + sb * 128u + col0;
-                uint32_t s[64];
-                float mx = -INFINITY;
-                if (alive) alive = warp_wait(bar(kBarSFull + (int)sb), spar);
-                if (alive) {
-                    tc_fence_after();
-                    tmem_ld32_issue(s_addr, reinterpret_cast<uint32_t(&)[32]>(s[0]));
-                    tmem_ld32_issue(s_addr + 32u, reinterpret_cast<uint32_t(&)[32]>(s[32]));
-                    const uint32_t bads = *reinterpret_cast<volatile uint32_t *>(smem + kOffBad + (tt & 7u) * 8u + 4u * (uint32_t)wg);
-                    tmem_ld_wait(reinterpret_cast<uint32_t(&)[32]>(s[0]));
-                    tmem_ld_wait(reinterpret_cast<uint32_t(&)[32]>(s[32]));
-                    const int32_t kidx0 = (int32_t)(t * (uint32_t)kTile + col0);
-                    if (bads != 0u) {
-#pragma unroll
-                        for (int b = 0; b < 4; ++b)
-                            if (((bads >> (8 * b)) & 1u) && kidx0 + 16 * b <= limit) marked = true;
-                    }
-                    if (!masked || kidx0 + 63 <= limit) {
-#pragma unroll
-                        for (int k = 0; k < 64; k += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(s[k]), __uint_as_float(s[k + 1])));
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 64; ++k) {
-                            if (kidx0 + k <= limit) mx = fmaxf(mx, __uint_as_float(s[k]));
-                            else s[k] = 0xFF800000u;
-                        }
-                    }
-                    mx *= p.scale_log2;
-                }
+            for (uint32_t t = 0; t < u.n_tiles; ++t, ++uses, ++tiles) {
+                if (alive) alive = warp_wait(kBarSFull + (int)x, uses & 1u);
                 if (!alive) continue;
+                tc_fence_after();
+                const int32_t seen = limit - (int32_t)(t * (uint32_t)kTile);   // the last key of the tile this row sees
+                const uint32_t meta = base + kOffMeta + (tiles & 7u) * 128u;
+                auto meta_of = [&](int b) {
+                    float4 v;
+                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(meta + 16u * (uint32_t)b));
+                    return v;
+                };
+                // scores of keys that the row does not see (whatever stands there): -inf.  Few tiles have any; the warp decides
+                // together, so that the others pay one vote per 32.
+                auto hide = [&](uint32_t (&v)[32], int first) {
+                    if (!__any_sync(0xffffffffu, seen < first + 31)) return;
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (first + k > seen) v[k] = 0xFF800000u;
+                };
+                float mx = -INFINITY;
+                uint32_t s[2][32];
+                tmem_ld32_issue(s_addr, s[0]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t(&v)[32] = s[c & 1];
+                    tmem_ld_wait(v);
+                    if (c < 3) tmem_ld32_issue(s_addr + 32u * (uint32_t)(c + 1), s[(c + 1) & 1]);
+                    hide(v, 32 * c);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const float4 mt = meta_of(2 * c + y);
+                        const uint32_t *r = v + 16 * y;
+                        float a = max3(__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[2]));
+                        float b = max3(__uint_as_float(r[3]), __uint_as_float(r[4]), __uint_as_float(r[5]));
+                        a = max3(a, __uint_as_float(r[6]), __uint_as_float(r[7]));
+                        b = max3(b, __uint_as_float(r[8]), __uint_as_float(r[9]));
+                        a = max3(a, __uint_as_float(r[10]), __uint_as_float(r[11]));
+                        b = max3(b, __uint_as_float(r[12]), __uint_as_float(r[13]));
+                        a = max3(a, __uint_as_float(r[14]), __uint_as_float(r[15]));
+                        // (a key block without a scale: a NaN, which takes no part in the maximum and stays in the sums)
+                        mx = fmaxf(mx, fmaxf(a, b) * (f_row * mt.x));
+                        if (mt.w != 0.f && 32 * c + 16 * y <= seen) marked = true;
+                    }
+                }
+                tmem_ld32_issue(s_addr, s[0]);
                 if (fresh) {
                     m_run = mx;
                     fresh = false;
                 } else if (__any_sync(0xffffffffu, mx > m_run + kRescaleStep)) {
-                    // a row of this warp has outgrown its reference: all of them move up and rescale (cart_shared.cu)
+                    // a row of this warp has outgrown its reference: all of them move up and rescale.  (P V of the tile before
+                    // is complete: its product was issued before these scores', whose completion has been waited for.)
                     const float m_new = fmaxf(m_run, mx);
                     const float f = m_new == -INFINITY ? 1.f : fast_exp2(m_run - m_new);
                     m_run = m_new;
                     l_run *= f;
-                    alive = warp_wait(bar(kBarSFree + (int)((tt - 1u) % (uint32_t)kSBufs)), ((tt - 1u) / (uint32_t)kSBufs) & 1u);
-                    if (!alive) continue;
-                    tc_fence_after();
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        uint32_t o[32];
-                        tmem_ld32_issue(o_addr + (uint32_t)c * 32u, o);
-                        tmem_ld_wait(o);
+                        tmem_ld32_issue(o_addr + (uint32_t)c * 32u, s[1]);
+                        tmem_ld_wait(s[1]);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                        tmem_st16(o_addr + (uint32_t)c * 32u, reinterpret_cast<const uint32_t(&)[16]>(o[0]));
-                        tmem_st16(o_addr + (uint32_t)c * 32u + 16u, reinterpret_cast<const uint32_t(&)[16]>(o[16]));
+                        for (int k = 0; k < 32; ++k) s[1][k] = __float_as_uint(__uint_as_float(s[1][k]) * f);
+                        tmem_st16(o_addr + (uint32_t)c * 32u, reinterpret_cast<const uint32_t(&)[16]>(s[1][0]));
+                        tmem_st16(o_addr + (uint32_t)c * 32u + 16u, reinterpret_cast<const uint32_t(&)[16]>(s[1][16]));
                     }
                 }
-                // probabilities as bf16 pairs, in the stored order of the tokens: pair 2 i of a block of 16 holds tokens
-                // 2 i and 2 i + 1, pair 2 i + 1 tokens 2 i + 8 and 2 i + 9
-                float psum0 = 0.f, psum1 = 0.f;
+                // probabilities times their values' scales as bf16 pairs, in the stored order of the tokens: pair 2 i of a
+                // block of 16 holds tokens 2 i and 2 i + 1, pair 2 i + 1 tokens 2 i + 8 and 2 i + 9.  (P of 32 tokens takes 16
+                // columns: it never reaches scores that have not been read.)
                 const float m_use = m_run == -INFINITY ? 0.f : m_run;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t(&v)[32] = s[c & 1];
+                    tmem_ld_wait(v);
+                    if (c < 3) tmem_ld32_issue(s_addr + 32u * (uint32_t)(c + 1), s[(c + 1) & 1]);
+                    hide(v, 32 * c);
                     uint32_t w[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const int tok = 32 * c + 16 * (j >> 3) + 2 * ((j & 7) >> 1) + 8 * (j & 1);
-                        const float p0 = fast_exp2(fmaf(__uint_as_float(s[tok]), p.scale_log2, -m_use));
-                        const float p1 = fast_exp2(fmaf(__uint_as_float(s[tok + 1]), p.scale_log2, -m_use));
-                        psum0 += p0;
-                        psum1 += p1;
-                        w[j] = pack_bf16(p0, p1);
+                    for (int y = 0; y < 2; ++y) {
+                        const float4 mt = meta_of(2 * c + y);
+                        // (a block of which the row sees nothing may have no scale, or none at all: -inf stays -inf)
+                        const float cc = 32 * c + 16 * y > seen ? 1.f : f_row * mt.x, dd = mt.y - m_use;
+                        const uint64_t cc2 = pair(cc, cc), dd2 = pair(dd, dd);
+                        uint64_t sum = pair(0.f, 0.f);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int tok = 2 * (j >> 1) + 8 * (j & 1);
+                            float2 e = unpair(fma2(pair(__uint_as_float(v[16 * y + tok]), __uint_as_float(v[16 * y + tok + 1])), cc2, dd2));
+                            e.x = fast_exp2(e.x);
+                            e.y = fast_exp2(e.y);
+                            sum = add2(sum, pair(e.x, e.y));
+                            w[8 * y + j] = pack_bf16(e.x, e.y);
+                        }
+                        const float2 t2 = unpair(sum);
+                        l_run = fmaf(t2.x + t2.y, mt.z, l_run);
                     }
                     tmem_st16(s_addr + (uint32_t)c * 16u, w);
                 }
-                l_run += psum0 + psum1;
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kBarPReady + 2 * (int)sb + wg));
-                if (has_next) {
-                    if (t == t_reader) {
-                        valid_next = (uint32_t)i_reader < uq.n_readers;
-                        if (valid_next) batch_next = p.readers[uq.reader_begin + (uint32_t)i_reader];
-                    }
-                    if (t == t_load) load_q(uq.kv_head, batch_next, valid_next, (unit_no + 1u) & 1u);
-                    if (t == t_store) q_bad_next = store_q((unit_no + 1u) & 1u);
-                }
+                if (lane == 0) mbar_arrive(bar(kBarPReady + (int)x));
+                // the chain's query rows have been read for the last time (its last scores are here): the next one's come
+                if (!hold && t + 1u == u.n_tiles && uq_next < unit_end) f_next = bring_q(head_next, batch_next, on_next);
             }
-
-            // ---- the chain's end: the two halves of the row's keys meet and the rows leave ----------------
             if (hold) continue;
-            uint32_t o[64];
-            if (alive) alive = warp_wait(bar(kBarSFree + (int)((tt - 1u) % (uint32_t)kSBufs)), ((tt - 1u) / (uint32_t)kSBufs) & 1u);
-            softmax_bar_both();  // the exchange area is free: the unit before has been read
-            xchg[wg * 128 + row] = m_run;
-            {
-                const uint32_t rows = __ballot_sync(0xffffffffu, marked);
-                if (lane == 0) mark[4 * wg + sw] = rows;
-            }
-            softmax_bar_both();
-            float2 theirs;
-            theirs.x = xchg[(wg ^ 1) * 128 + row];
-            const bool nan_row = ((mark[sw] | mark[4 + sw]) >> lane) & 1u;
-            softmax_bar_both();
-            xchg[wg * 128 + row] = l_run;
-            softmax_bar_both();
-            theirs.y = xchg[(wg ^ 1) * 128 + row];
-            const float m_all = fmaxf(m_run, theirs.x);
-            // (a half that saw no key has reference -inf and weight 0; where neither half has a reference, both sums are 0 or
-            //  NaN and count as they are)
-            const float w_mine = m_run == m_all ? 1.f : fast_exp2(m_run - m_all);
-            const float w_theirs = theirs.x == m_all ? 1.f : fast_exp2(theirs.x - m_all);
-            const float w_a = wg == 0 ? w_mine : w_theirs, w_b = wg == 0 ? w_theirs : w_mine;
-            const float l = w_a * (wg == 0 ? l_run : theirs.y) + w_b * (wg == 0 ? theirs.y : l_run);
+
+            // ---- the chain's end: the rows leave --------------------------------------------------------------
+            if (alive) alive = warp_wait(kBarOFull + (int)x, (uses - 1u) & 1u);
             if (alive) {
                 tc_fence_after();
+                const float poison = marked ? __uint_as_float(0x7FC00000u) : 1.f;
+                // (a row that saw no key of the run leaves an empty partial: zeros with lse = -inf, no weight in the merge)
+                const float inv = l_run == 0.f ? 0.f : poison / l_run;
+                const size_t orow = (size_t)slot * p.n_q_heads + (size_t)u.kv_head * G + h;
+                __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + orow * kHeadDim;
+                float *part = p.part_o + ((size_t)slot * G + h) * kHeadDim;
+                uint32_t s[32];
+#pragma unroll 1
+                for (uint32_t c = 0; c < 4; ++c) {
+                    tmem_ld32_issue(o_addr + 32u * c, s);
+                    tmem_ld_wait(s);
+                    if (!valid) continue;
+                    if (direct) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t a[32], b[32];
-                    tmem_ld32_issue(lane_addr + kTmemO + col0 + 32u * (uint32_t)c, a);
-                    tmem_ld32_issue(lane_addr + kTmemO + 128u + col0 + 32u * (uint32_t)c, b);
-                    tmem_ld_wait(a);
-                    tmem_ld_wait(b);
+                        for (int k = 0; k < 2; ++k) {   // 32 bytes per store: a thread fills whole sectors
+                            uint32_t w[8];
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) o[32 * c + k] = __float_as_uint(w_a * __uint_as_float(a[k]) + w_b * __uint_as_float(b[k]));
+                            for (int j = 0; j < 8; ++j)
+                                w[j] = pack_bf16(__uint_as_float(s[16 * k + 2 * j]) * inv, __uint_as_float(s[16 * k + 2 * j + 1]) * inv);
+                            asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(dst + 32 * c + 16 * k), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                            asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(dst + 32 * c + 16 * k + 8), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(part + 32 * c + 8 * k),
+                                         "f"(__uint_as_float(s[8 * k]) * inv), "f"(__uint_as_float(s[8 * k + 1]) * inv),
+                                         "f"(__uint_as_float(s[8 * k + 2]) * inv), "f"(__uint_as_float(s[8 * k + 3]) * inv),
+                                         "f"(__uint_as_float(s[8 * k + 4]) * inv), "f"(__uint_as_float(s[8 * k + 5]) * inv),
+                                         "f"(__uint_as_float(s[8 * k + 6]) * inv), "f"(__uint_as_float(s[8 * k + 7]) * inv)
+                                         : "memory");
+                    }
                 }
                 tc_fence_before();
-            }
-            const float poison = nan_row ? __uint_as_float(0x7FC00000u) : 1.f;
-            if (alive && valid && direct) {
-                const float inv = poison / l;
-                const size_t orow = (size_t)slot * p.n_q_heads + (size_t)u.kv_head * G + h;
-                __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + orow * kHeadDim + col0;
-#pragma unroll
-                for (int c16 = 0; c16 < 4; ++c16) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        w[j] = pack_bf16(__uint_as_float(o[16 * c16 + 2 * j]) * inv, __uint_as_float(o[16 * c16 + 2 * j + 1]) * inv);
-                    asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(dst + 16 * c16), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                    asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(dst + 16 * c16 + 8), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+                if (valid) {
+                    const float lse2 = l_run == 0.f ? -INFINITY : m_run + log2f(l_run);
+                    // (a row whose keys are all NaN has no reference; its sum is NaN, and so is this)
+                    if (!direct) p.part_lse2[(size_t)slot * kMaxGroup + h] = lse2;
+                    else if (p.lse) p.lse[orow] = lse2 * 0.6931471805599453f;
                 }
-                if (wg == 0 && p.lse) p.lse[orow] = (m_all + log2f(l)) * 0.6931471805599453f;
-            } else if (alive && valid) {
-                // (a row that saw no key of the run leaves an empty partial: zeros with lse = -inf, no weight in the merge)
-                const float inv = l == 0.f ? 0.f : poison / l;
-                float *dst = p.part_o + ((size_t)slot * G + h) * kHeadDim + col0;
-#pragma unroll
-                for (int q4 = 0; q4 < 16; ++q4)
-                    asm volatile("st.global.v4.f32 [%0], {%1,%2,%3,%4};" ::"l"(dst + 4 * q4), "f"(__uint_as_float(o[4 * q4]) * inv),
-                                 "f"(__uint_as_float(o[4 * q4 + 1]) * inv), "f"(__uint_as_float(o[4 * q4 + 2]) * inv),
-                                 "f"(__uint_as_float(o[4 * q4 + 3]) * inv)
-                                 : "memory");
-                if (wg == 0) p.part_lse2[(size_t)slot * kMaxGroup + h] = l == 0.f ? -INFINITY : m_all + log2f(l);
             }
         }
     }
 
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) {
+    if (warp == 0) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
