@@ -6,10 +6,10 @@
 // one another form a chain, over which the rows' softmax state carries on.  Per tile and M-tile: S = Q K^T, P = 2^(s - m),
 // O += P V, all three in tensor memory (P over the scores it came from).
 //
-//   4 converter warps  A tile is 32 KB of codes that become 64 KB of operands in shared memory.  Each warp takes two
-//                      blocks of 16 tokens of every tile, keys and values: 16-byte loads from global memory (a lane's
-//                      bytes of the stored order), codes to fp16 (keys) or bf16 (values), both exact and without the
-//                      blocks' scales, 8-byte stores into the swizzled tiles.  The next loads are in flight meanwhile.
+//   8 converter warps  A tile is 32 KB of codes that become 64 KB of operands in shared memory.  Each warp takes a block
+//                      of 16 tokens of every tile, keys and values: 16-byte loads from global memory (a lane's bytes of
+//                      the stored order), codes to fp16 (keys) or bf16 (values), both exact and without the blocks'
+//                      scales, 8-byte stores into the swizzled tiles.  The next loads are in flight meanwhile.
 //                      No raw tile is staged in shared memory: its bandwidth is what the products need (per tile and
 //                      pair of M-tiles 192 KB of operands are read and 64 KB written, as long as the products take).
 //   MMA warp           one thread issues, in turns, P V of one M-tile and the next S of the same, so that one M-tile's
@@ -27,8 +27,9 @@
 // (Blocks beyond 2^+-60 have their codes scaled to there by the converters.)  The query rows are fp16 numbers over a
 // power of two of their own.
 //
-// Two M-tiles per converted tile halve the conversions per product: with one (the layout of cart_shared.cu, each softmax
-// warpgroup on half of a tile's tokens) a tile took 3.7 us, the converters' loads setting the pace.
+// Two M-tiles per converted tile halve the conversions per product.  The loops are kept short (rolled, each role's body
+// written once): unrolled they overflowed the instruction cache that the roles share -- a third of its requests missed --
+// and a tile of a pair of M-tiles took 5.7 us.
 // A block of values without a scale (a NaN was written into it) becomes zeros in the operand, since rows that do not see
 // it would otherwise catch its NaN through 0 * NaN; the rows that do see one of its tokens are marked and end as NaN.
 // Every wait is bounded, as in cart_shared.cu.
@@ -47,13 +48,13 @@ constexpr uint32_t kBlock = 128u * 128u;              // 128 rows x 128 bytes: o
 constexpr uint32_t kTileBytes = 2u * kBlock;          // 128 x 128 bf16
 constexpr int kKStages = 3;
 constexpr int kVStages = 2;
-constexpr int kConvWarps = 4;
-constexpr int kThreads = 512;                         // utility warpgroup (warp 0: MMA), 2 softmax warpgroups, converters
-// Registers per thread after the warpgroups have re-divided the launch's 512 x 128 = 65536:
-// 128 x 72 + 256 x 144 + 128 x 152 = 65536.
+constexpr int kConvWarps = 8;
+constexpr int kThreads = 640;                         // utility warpgroup (warp 0: MMA), 2 softmax and 2 converter warpgroups
+// Registers per thread after the warpgroups have re-divided the launch's 640 x 96 = 61440:
+// 128 x 72 + 256 x 128 + 256 x 72 = 60416.
 constexpr int kRegsUtility = 72;
-constexpr int kRegsSoftmax = 144;
-constexpr int kRegsConvert = 152;
+constexpr int kRegsSoftmax = 128;
+constexpr int kRegsConvert = 72;
 constexpr uint32_t kTmemCols = 512;                   // S_A S_B (scores, then P), O_A O_B: 128 fp32 columns each
 constexpr uint32_t kTmemO = 2u * 128u;
 constexpr float kRescaleStep = 8.f;
@@ -219,23 +220,23 @@ __device__ __forceinline__ uint2 to_f16(uint32_t r)
     }
     return o;
 }
-// Four stored codes -> four bf16 numbers, exact.
+// Four stored codes -> four bf16 numbers times a power of two (a pair of bf16), exact.
 template <int kFmt>
-__device__ __forceinline__ uint2 to_bf16(uint32_t r)
+__device__ __forceinline__ uint2 to_bf16(uint32_t r, uint32_t factor)
 {
     uint2 o;
     if (kFmt == CART_Q8_INT8) {
         // A byte u = code + 128 below the byte 0x43 reads, without its top bit, as the bf16 number 128 + (u mod 128); the
         // code is that less 128 if the top bit is set, less 256 if not.
         const uint32_t x = __byte_perm(r, 0x43434343u, 0x4140), y = __byte_perm(r, 0x43434343u, 0x4342);
-        o.x = bf162_sub(x & 0xFF7FFF7Fu, (x & 0xFF80FF80u) ^ 0x00800080u);
-        o.y = bf162_sub(y & 0xFF7FFF7Fu, (y & 0xFF80FF80u) ^ 0x00800080u);
+        o.x = bf162_mul(bf162_sub(x & 0xFF7FFF7Fu, (x & 0xFF80FF80u) ^ 0x00800080u), factor);
+        o.y = bf162_mul(bf162_sub(y & 0xFF7FFF7Fu, (y & 0xFF80FF80u) ^ 0x00800080u), factor);
     } else {
         // e4m3's exponent and mantissa bits, moved to the low end of bf16's exponent and the high end of its mantissa, are
         // the number times 2^-120, subnormals included.
         const uint32_t x = __byte_perm(r, 0u, 0x1404), y = __byte_perm(r, 0u, 0x3424);
-        o.x = bf162_mul(((x >> 4) & 0x07F007F0u) | (x & 0x80008000u), 0x7B807B80u);
-        o.y = bf162_mul(((y >> 4) & 0x07F007F0u) | (y & 0x80008000u), 0x7B807B80u);
+        o.x = bf162_mul(bf162_mul(((x >> 4) & 0x07F007F0u) | (x & 0x80008000u), 0x7B807B80u), factor);
+        o.y = bf162_mul(bf162_mul(((y >> 4) & 0x07F007F0u) | (y & 0x80008000u), 0x7B807B80u), factor);
     }
     return o;
 }
@@ -306,8 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 fresh = (u.flags & CART_UNIT_CONT) ? 0u : 1u;
             };
             unit();
-            uint32_t q_uses[2] = {0u, 0u};   // chains whose rows M-tile x has taken
-            uint32_t p_uses[2] = {0u, 0u};   // tiles whose probabilities M-tile x has delivered
+            uint32_t q_uses = 0, p_uses = 0;   // bit x: parity of the chains whose rows, of the tiles whose P, M-tile x has delivered
             uint32_t kst = 0, kpar = 0, vst = 0, vpar = 0;
             // S_x = Q_x K^T: S_x last held probabilities, which P V products issued earlier by this thread read
             auto issue_s = [&](uint32_t x) {
@@ -322,14 +322,43 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 product_ts(tmem + kTmemO + 128u * x, tmem + x * 128u, umma_desc(base + kOffV + vst * kTileBytes, 16, 1024), first ? 0u : 1u);
                 mma_commit(bar(kBarOFull + (int)x));
             };
-            // the next tile's scores for M-tile x, if there is one (its rows first, where a chain begins)
-            auto next_s = [&](uint32_t x, bool k_wait) -> bool {
-                if (fresh && t == 0u && !wait(kBarQReady + (int)x, q_uses[x]++ & 1u)) return false;
-                if (k_wait && !wait(kBarKFull + (int)kst, kpar)) return false;
-                issue_s(x);
-                return true;
-            };
-            auto next_tile = [&]() {
+            // In turns: P V of one M-tile's current tile, then the scores of its next one.  (Written once, for both M-tiles
+            // and for the first tile too: the three roles' loops share an instruction cache, see above.)
+            bool have = false;               // there is a current tile
+            uint32_t cur_two = 0, cur_first = 0;
+            while (ok && (have || ui < unit_end)) {
+                const bool more = ui < unit_end;
+                const uint32_t nxt_two = two, nxt_first = (t == 0u && fresh) ? 1u : 0u;
+                if (have) ok = wait(kBarVFull + (int)vst, vpar);
+#pragma unroll 1
+                for (uint32_t x = 0; x < 2 && ok; ++x) {
+                    if (have && (x == 0u || cur_two)) {
+                        ok = wait(kBarPReady + (int)x, (p_uses >> x) & 1u);
+                        if (!ok) break;
+                        p_uses ^= 1u << x;
+                        issue_pv(x, cur_first);
+                    }
+                    if (more && (x == 0u || nxt_two)) {
+                        if (nxt_first) {
+                            ok = wait(kBarQReady + (int)x, (q_uses >> x) & 1u);
+                            if (!ok) break;
+                            q_uses ^= 1u << x;
+                        }
+                        if (x == 0u) ok = wait(kBarKFull + (int)kst, kpar);
+                        if (!ok) break;
+                        issue_s(x);
+                    }
+                }
+                if (!ok) break;
+                if (have) {
+                    mma_commit(bar(kBarVEmpty + (int)vst));
+                    if (++vst == (uint32_t)kVStages) {
+                        vst = 0;
+                        vpar ^= 1u;
+                    }
+                }
+                have = more;
+                if (!more) break;
                 mma_commit(bar(kBarKEmpty + (int)kst));
                 if (++kst == (uint32_t)kKStages) {
                     kst = 0;
@@ -340,42 +369,8 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                     t = 0;
                     unit();
                 }
-            };
-            // the tile in front: how many M-tiles it has, whether it begins a chain
-            uint32_t cur_two = two, cur_first = fresh;
-            if (ui < unit_end) {
-                ok = next_s(0u, true);
-                if (ok && two) ok = next_s(1u, false);
-                if (ok) next_tile();
-                while (ok) {
-                    const bool more = ui < unit_end;
-                    const uint32_t nxt_two = two, nxt_first = (t == 0u && fresh) ? 1u : 0u;
-                    ok = wait(kBarVFull + (int)vst, vpar) && wait(kBarPReady, p_uses[0]++ & 1u);
-                    if (!ok) break;
-                    issue_pv(0u, cur_first);
-                    if (more) {
-                        ok = next_s(0u, true);
-                        if (!ok) break;
-                    }
-                    if (cur_two) {
-                        ok = wait(kBarPReady + 1, p_uses[1]++ & 1u);
-                        if (!ok) break;
-                        issue_pv(1u, cur_first);
-                    }
-                    mma_commit(bar(kBarVEmpty + (int)vst));
-                    if (++vst == (uint32_t)kVStages) {
-                        vst = 0;
-                        vpar ^= 1u;
-                    }
-                    if (!more) break;
-                    if (nxt_two) {
-                        ok = next_s(1u, false);
-                        if (!ok) break;
-                    }
-                    next_tile();
-                    cur_two = nxt_two;
-                    cur_first = nxt_first;
-                }
+                cur_two = nxt_two;
+                cur_first = nxt_first;
             }
             // products still in flight must finish before the tensor memory is given back
             mma_commit(bar(kBarDrain));
@@ -383,110 +378,98 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
             while (!mbar_try_wait(bar(kBarDrain), 0) && global_timer_ns() - t0 < kWaitLimitNs) {}
         }
     } else if (warp >= 12) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
         // ================= converters: codes -> bf16 operand tiles ======================================
-        // Warp w takes the blocks w and w + 4 of every tile (block w of either page), their keys and then their values.
+        // Warp w takes block w of every tile, its keys and then its values.
         const uint32_t b = (uint32_t)warp - 12u;
         const uint32_t g = (uint32_t)lane >> 2, t4 = (uint32_t)lane & 3u;
         pdl_wait();  // the codes may come from the kernel before
         // where the tile whose codes are requested next lies
-        uint32_t ui = unit_begin, t = 0, n = 0, row = 0, tok_end = 0;
-        uint32_t page[2] = {0u, 0u}, page_next[2] = {0u, 0u};   // base rows of its two pages, and of the next tile's
+        uint32_t ui = unit_begin, t = 0, n = 0, row = 0, tok_end = 0, page = 0, page_next = 0;
         const uint8_t *head = nullptr;   // the warp's block of the KV head, in a page at row 0
-        auto page_of = [&](uint32_t tile, uint32_t y) {   // (the list may end before the last tile's second page)
-            return tile < n && tile * (uint32_t)kTile + y * 64u < tok_end ? __ldg(p.pages + row + 2u * tile + y) : 0u;
+        auto page_of = [&](uint32_t tile) {   // (the list may end before the last tile's second page)
+            return tile < n && tile * (uint32_t)kTile + b * 16u < tok_end ? __ldg(p.pages + row + 2u * tile + (b >> 2)) : 0u;
         };
         auto unit = [&]() {
             if (ui >= unit_end) return;
             const cart_shared_unit u = p.units[ui];
             row = u.k_row;
-            head = p.arena + ((size_t)((uint32_t)p.layer * u.layer_stride + u.v_row) * (kTileTokens / kQ8Block) + b) * kQ8BlockBytes;
+            head = p.arena + ((size_t)((uint32_t)p.layer * u.layer_stride + u.v_row) * (kTileTokens / kQ8Block) + (b & 3u)) * kQ8BlockBytes;
             n = u.n_tiles;
             tok_end = (u.flags & CART_UNIT_MASKED) ? (uint32_t)(u.lim_cap + 1) : u.n_tiles * (uint32_t)kTile;
-#pragma unroll
-            for (uint32_t y = 0; y < 2; ++y) {
-                page[y] = page_of(0u, y);
-                page_next[y] = page_of(1u, y);
-            }
+            page = page_of(0u);
+            page_next = page_of(1u);
         };
         unit();
-        struct Codes { uint4 x[4]; };
-        // of the tile whose keys were requested last: scale bytes; tokens of the block that exist (may exceed 16)
-        uint32_t scales[2] = {0u, 0u}, left[2] = {0u, 0u};
-        const uint8_t *blk[2] = {nullptr, nullptr};
-        auto load = [&](Codes &k, const uint8_t *at) {
-            const uint4 *src = reinterpret_cast<const uint4 *>(at) + lane;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) k.x[c] = __ldcg(src + 32 * c);
-        };
+        // Lanes of odd g hold the chunks 1 0 3 2 of the keys instead of 0 1 2 3: the 8-byte stores of a half warp then fall
+        // on all banks (with all lanes at the same dims, on half of them).
+        const uint32_t odd = g & 1u;
+        uint4 ck[4], cv[4];
+        uint32_t scales = 0, left = 0;   // of the tile whose keys were requested last: scale bytes; tokens of the block (may exceed 16)
+        const uint8_t *blk = nullptr;
         // requests the keys of the next tile; false: there is none
-        auto next_keys = [&](Codes (&k)[2]) -> bool {
+        auto next_keys = [&]() -> bool {
             if (ui >= unit_end) return false;
+            const uint32_t tok = t * (uint32_t)kTile + b * 16u;
+            left = tok < tok_end ? tok_end - tok : 0u;
+            scales = 0u;
+            if (left > 0u) {
+                blk = head + (size_t)page * kRowBytes;
+                const uint4 *src = reinterpret_cast<const uint4 *>(blk) + lane;
 #pragma unroll
-            for (uint32_t y = 0; y < 2; ++y) {
-                const uint32_t tok = t * (uint32_t)kTile + y * 64u + b * 16u;
-                left[y] = tok < tok_end ? tok_end - tok : 0u;
-                scales[y] = 0u;
-                if (left[y] > 0u) {
-                    blk[y] = head + (size_t)page[y] * kRowBytes;
-                    load(k[y], blk[y]);
-                    scales[y] = __ldcg(reinterpret_cast<const unsigned short *>(blk[y] + kQ8ScaleOff));
-                }
-                page[y] = page_next[y];
+                for (uint32_t c = 0; c < 4; ++c) ck[c] = __ldcg(src + 32u * (c ^ odd));
+                scales = __ldcg(reinterpret_cast<const unsigned short *>(blk + kQ8ScaleOff));
             }
+            page = page_next;
             if (++t == n) {
                 ++ui;
                 t = 0;
                 unit();
             } else {
-                page_next[0] = page_of(t + 1u, 0u);
-                page_next[1] = page_of(t + 1u, 1u);
+                page_next = page_of(t + 1u);
             }
             return true;
         };
-        Codes ck[2], cv[2];
-        bool ok = true, more = next_keys(ck);
+        bool ok = true, more = next_keys();
         uint32_t kst = 0, kpar = 1, vst = 0, vpar = 1, tt = 0;
         auto wait_conv = [&](int x, uint32_t parity) -> bool {
             return __all_sync(0xffffffffu, mbar_wait(bar(x), parity, abort_flag, p.status, kStatusTimeoutProducer));
         };
-        // 8-byte stores: word (c, j) of a lane goes to row 64 y + 16 b + g + 8 (j & 1) [keys], dims 16 (2 c + j / 2) + 4 t4 ..;
-        // or [values] to dim 16 (2 c + j / 2) + g + 8 (j & 1), stored tokens 64 y + 16 b + 4 t4 ..
-        const uint32_t k_at = (16u * b + g) * 128u + (t4 & 1u) * 8u;
-        const uint32_t v_at = g * 128u + (((2u * b + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u;
-        while (more) {
-            uint32_t cur_scales[2], cur_left[2];
+        // 8-byte stores: word (c, j) of a lane goes to row 16 b + g + 8 (j & 1) [keys], dims 16 ks + 4 t4 .. with ks = 2 (c ^ odd) +
+        // j / 2; or [values] to dim 16 (2 c + j / 2) + g + 8 (j & 1), stored tokens 16 b + 4 t4 ..
+        uint32_t k_at[2][2];   // [c & 1][j / 2]
 #pragma unroll
-            for (uint32_t y = 0; y < 2; ++y) {
-                cur_scales[y] = scales[y];
-                cur_left[y] = left[y];
-                if (cur_left[y] > 0u) load(cv[y], blk[y] + kQ8ValueOff);
+        for (uint32_t c = 0; c < 2; ++c)
+#pragma unroll
+            for (uint32_t j = 0; j < 2; ++j)
+                k_at[c][j] = base + kOffK + (16u * b + g) * 128u + (((2u * (2u * (c ^ odd) + j) + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u;
+        const uint32_t v_at = base + kOffV + (b >> 2) * kBlock + g * 128u + (((2u * (b & 3u) + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u;
+        while (more) {
+            const uint32_t cur_scales = scales, cur_left = left;
+            if (cur_left > 0u) {
+                const uint4 *src = reinterpret_cast<const uint4 *>(blk + kQ8ValueOff) + lane;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) cv[c] = __ldcg(src + 32 * c);
             }
+            const uint32_t ek = cur_scales & 0xFFu, ev = cur_scales >> 8;
+            const bool none = cur_left == 0u || ev == kQ8NoScale;   // no values here: zeros
+            const int fold = none ? 0 : min(max((int)ev - 127, -kFoldExp), kFoldExp);
             ok = wait_conv(kBarKEmpty + (int)kst, kpar);
             if (!ok) break;
-#pragma unroll
-            for (uint32_t y = 0; y < 2; ++y) {
-                if (lane == 0) {
-                    const uint32_t ek = cur_scales[y] & 0xFFu, ev = cur_scales[y] >> 8;
-                    const bool none = cur_left[y] == 0u || ev == kQ8NoScale;
-                    const int fold = none ? 0 : min(max((int)ev - 127, -kFoldExp), kFoldExp);
-                    // (a block without tokens: no scale is read, its scores are masked)
-                    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + kOffMeta + ((tt & 7u) * 8u + 4u * y + b) * 16u),
-                                 "f"(ek == kQ8NoScale ? __uint_as_float(0x7FC00000u) : __uint_as_float(ek << 23)), "f"((float)fold),
-                                 "f"(__uint_as_float((uint32_t)(127 - fold) << 23)), "f"(cur_left[y] > 0u && ev == kQ8NoScale ? 1.f : 0.f)
-                                 : "memory");
-                }
-                if (cur_left[y] == 0u) continue;   // (scores of keys that do not exist are masked, whatever stands there)
-                const uint32_t dst = base + kOffK + kst * kTileBytes + y * (kBlock / 2u) + k_at;
+            if (lane == 0)   // (a block without tokens: its scores are masked, whatever the scale)
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + kOffMeta + ((tt & 7u) * 8u + b) * 16u),
+                             "f"(ek == kQ8NoScale ? __uint_as_float(0x7FC00000u) : __uint_as_float(ek << 23)), "f"((float)fold),
+                             "f"(__uint_as_float((uint32_t)(127 - fold) << 23)), "f"(cur_left > 0u && ev == kQ8NoScale ? 1.f : 0.f)
+                             : "memory");
+            if (cur_left > 0u) {   // (scores of keys that do not exist are masked, whatever stands there)
+                const uint32_t dst = kst * kTileBytes;
 #pragma unroll
                 for (uint32_t c = 0; c < 4; ++c) {
-                    const uint32_t w[4] = {ck[y].x[c].x, ck[y].x[c].y, ck[y].x[c].z, ck[y].x[c].w};
+                    const uint32_t w[4] = {ck[c].x, ck[c].y, ck[c].z, ck[c].w};
 #pragma unroll
                     for (uint32_t j = 0; j < 4; ++j) {
-                        const uint32_t ks = 2u * c + (j >> 1);
                         const uint2 v = to_f16<kFmt>(w[j]);
-                        asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(dst + (ks >> 2) * kBlock + (j & 1u) * 1024u +
-                                                                             (((2u * (ks & 3u) + (t4 >> 1)) ^ g) << 4)),
+                        asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(k_at[c & 1u][j >> 1] + dst + (c >> 1) * kBlock + (j & 1u) * 1024u),
                                      "r"(v.x), "r"(v.y)
                                      : "memory");
                     }
@@ -499,38 +482,29 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 kst = 0;
                 kpar ^= 1u;
             }
-            more = next_keys(ck);
+            more = next_keys();
             ok = wait_conv(kBarVEmpty + (int)vst, vpar);
             if (!ok) break;
+            uint32_t m0 = 0xFFFFFFFFu, m1 = 0xFFFFFFFFu;   // tokens behind the end count as zeros
+            if (none) {
+                m0 = m1 = 0u;
+            } else if (cur_left < 16u) {
+                m0 = (2u * t4 < cur_left ? 0xFFFFu : 0u) | (2u * t4 + 1u < cur_left ? 0xFFFF0000u : 0u);
+                m1 = (2u * t4 + 8u < cur_left ? 0xFFFFu : 0u) | (2u * t4 + 9u < cur_left ? 0xFFFF0000u : 0u);
+            }
+            // (a scale beyond what the probabilities carry)
+            const uint32_t over = none ? 127u : (uint32_t)((int)ev - fold);
+            const uint32_t extra = over << 7 | over << 23;
+            const uint32_t dst = v_at + vst * kTileBytes;
 #pragma unroll
-            for (uint32_t y = 0; y < 2; ++y) {
-                const uint32_t eb = cur_scales[y] >> 8;
-                const bool none = cur_left[y] == 0u || eb == kQ8NoScale;
-                // (beyond what the probabilities carry)
-                const int over = none ? 0 : (int)eb - 127 - min(max((int)eb - 127, -kFoldExp), kFoldExp);
-                const uint32_t extra = (uint32_t)(127 + over) << 7, extra2 = extra | extra << 16;
-                uint32_t m0 = 0xFFFFFFFFu, m1 = 0xFFFFFFFFu;   // tokens behind the end count as zeros
-                if (none) {
-                    m0 = m1 = 0u;
-                } else if (cur_left[y] < 16u) {
-                    m0 = (2u * t4 < cur_left[y] ? 0xFFFFu : 0u) | (2u * t4 + 1u < cur_left[y] ? 0xFFFF0000u : 0u);
-                    m1 = (2u * t4 + 8u < cur_left[y] ? 0xFFFFu : 0u) | (2u * t4 + 9u < cur_left[y] ? 0xFFFF0000u : 0u);
-                }
-                const uint32_t dst = base + kOffV + vst * kTileBytes + y * kBlock + v_at;
+            for (uint32_t c = 0; c < 4; ++c) {
+                const uint32_t w[4] = {cv[c].x, cv[c].y, cv[c].z, cv[c].w};
 #pragma unroll
-                for (uint32_t c = 0; c < 4; ++c) {
-                    const uint32_t w[4] = {cv[y].x[c].x, cv[y].x[c].y, cv[y].x[c].z, cv[y].x[c].w};
-#pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j) {
-                        uint2 v = to_bf16<kFmt>(w[j]);
-                        if (over != 0) {
-                            v.x = bf162_mul(v.x, extra2);
-                            v.y = bf162_mul(v.y, extra2);
-                        }
-                        asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(dst + (2u * c + (j >> 1)) * 2048u + (j & 1u) * 1024u),
-                                     "r"(v.x & m0), "r"(v.y & m1)
-                                     : "memory");
-                    }
+                for (uint32_t j = 0; j < 4; ++j) {
+                    const uint2 v = to_bf16<kFmt>(w[j], extra);
+                    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(dst + (2u * c + (j >> 1)) * 2048u + (j & 1u) * 1024u), "r"(v.x & m0),
+                                 "r"(v.y & m1)
+                                 : "memory");
                 }
             }
             fence_async_smem();
@@ -682,11 +656,14 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 float mx = -INFINITY;
                 uint32_t s[2][32];
                 tmem_ld32_issue(s_addr, s[0]);
+#pragma unroll 1
+                for (int c2 = 0; c2 < 4; c2 += 2)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t(&v)[32] = s[c & 1];
+                for (int z = 0; z < 2; ++z) {
+                    const int c = c2 + z;
+                    uint32_t(&v)[32] = s[z];
                     tmem_ld_wait(v);
-                    if (c < 3) tmem_ld32_issue(s_addr + 32u * (uint32_t)(c + 1), s[(c + 1) & 1]);
+                    if (z == 0 || c2 == 0) tmem_ld32_issue(s_addr + 32u * (uint32_t)(c + 1), s[z ^ 1]);
                     hide(v, 32 * c);
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
@@ -715,7 +692,7 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                     const float f = m_new == -INFINITY ? 1.f : fast_exp2(m_run - m_new);
                     m_run = m_new;
                     l_run *= f;
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         tmem_ld32_issue(o_addr + (uint32_t)c * 32u, s[1]);
                         tmem_ld_wait(s[1]);
@@ -729,11 +706,14 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 // block of 16 holds tokens 2 i and 2 i + 1, pair 2 i + 1 tokens 2 i + 8 and 2 i + 9.  (P of 32 tokens takes 16
                 // columns: it never reaches scores that have not been read.)
                 const float m_use = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll 1
+                for (int c2 = 0; c2 < 4; c2 += 2)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t(&v)[32] = s[c & 1];
+                for (int z = 0; z < 2; ++z) {
+                    const int c = c2 + z;
+                    uint32_t(&v)[32] = s[z];
                     tmem_ld_wait(v);
-                    if (c < 3) tmem_ld32_issue(s_addr + 32u * (uint32_t)(c + 1), s[(c + 1) & 1]);
+                    if (z == 0 || c2 == 0) tmem_ld32_issue(s_addr + 32u * (uint32_t)(c + 1), s[z ^ 1]);
                     hide(v, 32 * c);
                     uint32_t w[16];
 #pragma unroll
