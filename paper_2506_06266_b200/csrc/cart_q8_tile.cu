@@ -12,14 +12,16 @@
 //                      scales, 8-byte stores into the swizzled tiles.  The next loads are in flight meanwhile.
 //                      No raw tile is staged in shared memory: its bandwidth is what the products need (per tile and
 //                      pair of M-tiles 192 KB of operands are read and 64 KB written, as long as the products take).
-//   MMA warp           one thread issues, in turns, P V of one M-tile and the next S of the same, so that one M-tile's
-//                      products run while the other's softmax does.  V is a K-major operand [dim][token], because a word
-//                      of the stored values holds four tokens of one dim; inside a block of 16 the tokens stand in the
-//                      stored order 0 1 8 9  2 3 10 11  4 5 12 13  6 7 14 15, and the softmax threads pack their
-//                      probabilities in that order, which costs nothing.
-//   2 x 4 softmax      one warpgroup per M-tile, one thread per row.  The scores are read twice from tensor memory (for
-//   warps              the maximum, then for the exponentials), which leaves the registers to the converters.  A row's
-//                      reference m moves only when outgrown by more than 2^8; its thread then rescales the accumulator.
+//   MMA thread         A tile's keys are dealt with in halves: S of 64 keys, its softmax, P V of these 64 tokens.  As soon as
+//                      a half's P is there, its P V is issued and behind it S of the same half of the next tile, into the
+//                      same columns; the softmax meanwhile has the other half.  So neither waits for the other's latency
+//                      (with whole tiles a row's softmax, P V and S took turns: 6000 cycles a tile, 2048 of them
+//                      exponentials).  V is a K-major operand [dim][token], because a word of the stored values holds four
+//                      tokens of one dim; inside a block of 16 the tokens stand in the stored order 0 1 8 9  2 3 10 11
+//                      4 5 12 13  6 7 14 15, and the softmax threads pack their probabilities in that order, which costs
+//                      nothing.
+//   2 x 4 softmax      one warpgroup per M-tile, one thread per row.  A row's reference m moves only when outgrown by more
+//   warps              than 2^8; its thread then rescales the accumulator.
 //
 // The scales join the softmax, where a block's 16 tokens are 16 columns of a thread's row: keys' scales multiply the
 // scores (in place of the softmax's own factor), values' scales are added in the exponent, so that P is held times the
@@ -51,9 +53,9 @@ constexpr int kVStages = 2;
 constexpr int kConvWarps = 8;
 constexpr int kThreads = 640;                         // utility warpgroup (warp 0: MMA), 2 softmax and 2 converter warpgroups
 // Registers per thread after the warpgroups have re-divided the launch's 640 x 96 = 61440:
-// 128 x 72 + 256 x 128 + 256 x 72 = 60416.
-constexpr int kRegsUtility = 72;
-constexpr int kRegsSoftmax = 128;
+// 128 x 56 + 256 x 136 + 256 x 72 = 60416.
+constexpr int kRegsUtility = 56;
+constexpr int kRegsSoftmax = 136;
 constexpr int kRegsConvert = 72;
 constexpr uint32_t kTmemCols = 512;                   // S_A S_B (scores, then P), O_A O_B: 128 fp32 columns each
 constexpr uint32_t kTmemO = 2u * 128u;
@@ -77,23 +79,23 @@ enum Bar : int {
     kBarKEmpty = 3,  // [kKStages] MMA (commit of the tile's last score product) -> converters
     kBarVFull = 6,   // [kVStages]
     kBarVEmpty = 8,  // [kVStages] MMA (commit of the tile's last P V product) -> converters
-    kBarSFull = 10,  // [M-tile] MMA (commit, and an arrival that passes the converters' scales on) -> softmax: the scores are
-                     // there, and so is P V of the tile before
-    kBarPReady = 12, // [M-tile] softmax -> MMA (4 arrivals: one per warp)
-    kBarQReady = 14, // [M-tile] softmax -> MMA: a chain's query rows are in place (4 arrivals)
-    kBarOFull = 16,  // [M-tile] MMA (commit of P V) -> softmax
-    kBarDrain = 18,  // MMA (commit) -> MMA, on the way out
+    kBarSFull = 10,  // [M-tile][half] MMA (commit, and an arrival that passes the converters' scales on) -> softmax: the
+                     // scores are there, and so is P V of the same half of the tile before
+    kBarPReady = 14, // [M-tile][half] softmax -> MMA (4 arrivals: one per warp)
+    kBarQReady = 18, // [M-tile] softmax -> MMA: a chain's query rows are in place (4 arrivals)
+    kBarOFull = 20,  // [M-tile][half] MMA (commit of P V) -> softmax.  (A barrier per half: whoever waits for one has seen
+                     // scores that were issued behind the phase before, so its parity is not ambiguous.)
+    kBarDrain = 24,  // MMA (commit) -> MMA, on the way out
 };
 
-// Instruction descriptors: fp32 accumulator, both operands K-major, M = 128, N = 128; fp16 (S) or bf16 (P V).
+// Instruction descriptors: fp32 accumulator, both operands K-major, M = 128; fp16, N = 64 (S), or bf16, N = 128 (P V).
 constexpr uint32_t kIdescPV = umma_idesc_bf16(128u, 128u, false, false);
-constexpr uint32_t kIdescS = kIdescPV & ~((1u << 7) | (1u << 10));
+constexpr uint32_t kIdescS = umma_idesc_bf16(128u, 64u, false, false) & ~((1u << 7) | (1u << 10));
 
-// The eight instructions of a product (16 dims or tokens each; the operands' descriptors differ in their start address
-// only: 32 bytes per step, the second 64-element block kBlock on), issued by one thread.  D = A B, or with `accumulate`
-// D += A B.
+// S of 64 keys: eight instructions of 16 dims (the descriptors differ in their start address only: 32 bytes per step, the
+// second 64-dim block kBlock on); P V of 64 tokens: four of 16 tokens.  Issued by one thread.
 static_assert(kBlock == 16384u, "the steps' offsets below");
-__device__ __forceinline__ void product_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc)
+__device__ __forceinline__ void product_s(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc)
 {
     asm volatile(
         "{\n"
@@ -129,7 +131,7 @@ __device__ __forceinline__ void product_ss(uint32_t d_tmem, uint64_t a_desc, uin
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(kIdescS), "r"(0u)
         : "memory");
 }
-__device__ __forceinline__ void product_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t accumulate)
+__device__ __forceinline__ void product_pv(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t accumulate)
 {
     asm volatile(
         "{\n"
@@ -145,14 +147,6 @@ __device__ __forceinline__ void product_ts(uint32_t d_tmem, uint32_t a_tmem, uin
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 16], b, %3, p;\n"
         "add.s64 b, %2, 6;\n"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 24], b, %3, p;\n"
-        "add.s64 b, %2, 1024;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 32], b, %3, p;\n"
-        "add.s64 b, %2, 1026;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 40], b, %3, p;\n"
-        "add.s64 b, %2, 1028;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 48], b, %3, p;\n"
-        "add.s64 b, %2, 1030;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1 + 56], b, %3, p;\n"
         "}\n"
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(kIdescPV), "r"(accumulate)
         : "memory");
@@ -160,6 +154,16 @@ __device__ __forceinline__ void product_ts(uint32_t d_tmem, uint32_t a_tmem, uin
 __device__ __forceinline__ void mma_commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
 }
 // pairs of fp32
 __device__ __forceinline__ uint64_t pair(float a, float b)
@@ -269,12 +273,12 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
             mbar_init(bar(kBarVFull + i), kConvWarps);
             mbar_init(bar(kBarVEmpty + i), 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             mbar_init(bar(kBarSFull + i), 2);
             mbar_init(bar(kBarPReady + i), 4);
-            mbar_init(bar(kBarQReady + i), 4);
             mbar_init(bar(kBarOFull + i), 1);
         }
+        for (int i = 0; i < 2; ++i) mbar_init(bar(kBarQReady + i), 4);
         mbar_init(bar(kBarDrain), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -307,46 +311,40 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 fresh = (u.flags & CART_UNIT_CONT) ? 0u : 1u;
             };
             unit();
-            uint32_t q_uses = 0, p_uses = 0;   // bit x: parity of the chains whose rows, of the tiles whose P, M-tile x has delivered
+            uint32_t q_uses = 0, p_uses = 0;   // bit x: parity of the chains whose rows, and of the tiles whose P, M-tile x has delivered
             uint32_t kst = 0, kpar = 0, vst = 0, vpar = 0;
-            // S_x = Q_x K^T: S_x last held probabilities, which P V products issued earlier by this thread read
-            auto issue_s = [&](uint32_t x) {
+            // S of half y of the tile in front for M-tile x: its columns last held P, which a P V product issued earlier reads
+            auto issue_s = [&](uint32_t x, uint32_t y) {
                 tc_fence_after();
-                product_ss(tmem + x * 128u, umma_desc(base + kOffQ + x * kTileBytes, 16, 1024), umma_desc(base + kOffK + kst * kTileBytes, 16, 1024));
-                mma_commit(bar(kBarSFull + (int)x));
-                mbar_arrive(bar(kBarSFull + (int)x));
+                product_s(tmem + x * 128u + y * 64u, umma_desc(base + kOffQ + x * kTileBytes, 16, 1024),
+                          umma_desc(base + kOffK + kst * kTileBytes + y * (kBlock / 2u), 16, 1024));
+                mma_commit(bar(kBarSFull + (int)(2u * x + y)));
+                mbar_arrive(bar(kBarSFull + (int)(2u * x + y)));
             };
-            // O_x += P_x V (O_x = P_x V for a chain's first tile)
-            auto issue_pv = [&](uint32_t x, uint32_t first) {
-                tc_fence_after();
-                product_ts(tmem + kTmemO + 128u * x, tmem + x * 128u, umma_desc(base + kOffV + vst * kTileBytes, 16, 1024), first ? 0u : 1u);
-                mma_commit(bar(kBarOFull + (int)x));
-            };
-            // In turns: P V of one M-tile's current tile, then the scores of its next one.  (Written once, for both M-tiles
-            // and for the first tile too: the three roles' loops share an instruction cache, see above.)
+            // (Written once, for both M-tiles and halves and for the first tile too: the roles share an instruction cache.)
             bool have = false;               // there is a current tile
             uint32_t cur_two = 0, cur_first = 0;
             while (ok && (have || ui < unit_end)) {
                 const bool more = ui < unit_end;
                 const uint32_t nxt_two = two, nxt_first = (t == 0u && fresh) ? 1u : 0u;
                 if (have) ok = wait(kBarVFull + (int)vst, vpar);
+                // the current tile's P V and, in the same chain, the next tile's S
+                bool k_here = false;
 #pragma unroll 1
-                for (uint32_t x = 0; x < 2 && ok; ++x) {
-                    if (have && (x == 0u || cur_two)) {
-                        ok = wait(kBarPReady + (int)x, (p_uses >> x) & 1u);
+                for (uint32_t z = 0; z < 4 && ok && have; ++z) {
+                    const uint32_t x = z & 1u, y = z >> 1;
+                    if (x == 1u && !cur_two) continue;
+                    ok = wait(kBarPReady + (int)(2u * x + y), (p_uses >> x) & 1u);
+                    if (!ok) break;
+                    tc_fence_after();
+                    product_pv(tmem + kTmemO + 128u * x, tmem + x * 128u + y * 64u, umma_desc(base + kOffV + vst * kTileBytes + y * kBlock, 16, 1024),
+                               (cur_first && y == 0u) ? 0u : 1u);
+                    mma_commit(bar(kBarOFull + (int)(2u * x + y)));
+                    if (more && !nxt_first) {
+                        if (!k_here) ok = wait(kBarKFull + (int)kst, kpar);
                         if (!ok) break;
-                        p_uses ^= 1u << x;
-                        issue_pv(x, cur_first);
-                    }
-                    if (more && (x == 0u || nxt_two)) {
-                        if (nxt_first) {
-                            ok = wait(kBarQReady + (int)x, (q_uses >> x) & 1u);
-                            if (!ok) break;
-                            q_uses ^= 1u << x;
-                        }
-                        if (x == 0u) ok = wait(kBarKFull + (int)kst, kpar);
-                        if (!ok) break;
-                        issue_s(x);
+                        k_here = true;
+                        issue_s(x, y);
                     }
                 }
                 if (!ok) break;
@@ -356,9 +354,22 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                         vst = 0;
                         vpar ^= 1u;
                     }
+                    p_uses ^= cur_two ? 3u : 1u;
                 }
                 have = more;
                 if (!more) break;
+                if (nxt_first) {   // a new chain: its rows first
+                    ok = wait(kBarKFull + (int)kst, kpar);
+#pragma unroll 1
+                    for (uint32_t x = 0; x < 1u + nxt_two && ok; ++x) {
+                        ok = wait(kBarQReady + (int)x, (q_uses >> x) & 1u);
+                        if (!ok) break;
+                        q_uses ^= 1u << x;
+                        issue_s(x, 0u);
+                        issue_s(x, 1u);
+                    }
+                    if (!ok) break;
+                }
                 mma_commit(bar(kBarKEmpty + (int)kst));
                 if (++kst == (uint32_t)kKStages) {
                     kst = 0;
@@ -531,50 +542,55 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
         auto warp_wait = [&](int b, uint32_t parity) -> bool {
             return __all_sync(0xffffffffu, mbar_wait(bar(b), parity, abort_flag, p.status, kStatusTimeoutConsumer));
         };
-        // The row into the swizzled K-major operand -- block w (64 dims), 16-byte chunk c at position c ^ (row % 8) -- as fp16
-        // over the power of two that brings its largest value to 1 .. 2 (see cart_q8.cu); a row with a NaN or an infinity
-        // as NaN, rows past the readers as zeros.  Returns what takes its scores to base-2 exponents: 2^e scale log2(e).
-        const uint32_t q_row = base + kOffQ + x * kTileBytes + row * 128u;
-        auto q_src = [&](uint32_t kv_head, uint32_t batch) {
-            return reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) +
-                                                   ((size_t)batch * p.n_q_heads + (size_t)kv_head * G + h) * kHeadDim);
-        };
+        // A chain's rows into the swizzled K-major operand -- block w (64 dims), 16-byte chunk c at position c ^ (row % 8) -- as
+        // fp16 over the power of two that brings a row's largest value to 1 .. 2 (see cart_q8.cu); a row with a NaN or an
+        // infinity as NaN, rows past the readers as zeros.  The warp brings its 32 rows together, 16 lanes a row, eight rows'
+        // loads in flight.  Returns what takes the thread's own row's scores to base-2 exponents: 2^e scale log2(e).
+        const uint32_t q_base = base + kOffQ + x * kTileBytes + 32u * sw * 128u;
         auto bring_q = [&](uint32_t kv_head, uint32_t batch, bool on) -> float {
-            const uint4 *src = q_src(kv_head, batch);
-            uint32_t big = 0u;
-            if (on) {
-#pragma unroll 8
-                for (uint32_t c = 0; c < 16; ++c) {
-                    const uint4 v = __ldg(src + c);
-                    big = __vmaxu2(big, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
+            const uint32_t c = (uint32_t)lane & 15u, up = (uint32_t)lane >> 4;
+            const uint32_t from = on ? batch * (uint32_t)p.n_q_heads + kv_head * G + h : ~0u;   // the row's place among all of q's
+            int my_exp = 0;
+#pragma unroll 1
+            for (uint32_t r0 = 0; r0 < 32u; r0 += 8u) {
+                uint4 v[4];
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint32_t src = __shfl_sync(0xffffffffu, from, (int)(r0 + 2u * i + up));
+                    v[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (src != ~0u) v[i] = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) + (size_t)src * kHeadDim) + c);
                 }
-                big = max(big & 0xFFFFu, big >> 16);
-            }
-            const int qe = big >= 0x7F80u ? 0 : min(max((int)(big >> 7), 2) - 127, 126);
-            const float down = big >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - qe) << 23);
-#pragma unroll 4
-            for (uint32_t c = 0; c < 16; ++c) {
-                uint32_t w[4] = {0u, 0u, 0u, 0u};
-                if (on) {
-                    const uint4 v = __ldg(src + c);
-                    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    uint32_t big = __vmaxu2(__vmaxu2(v[i].x & 0x7FFF7FFFu, v[i].y & 0x7FFF7FFFu), __vmaxu2(v[i].z & 0x7FFF7FFFu, v[i].w & 0x7FFF7FFFu));
+                    big = max(big & 0xFFFFu, big >> 16);
+#pragma unroll
+                    for (int d = 1; d < 16; d <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
+                    const int qe = big >= 0x7F80u ? 0 : min(max((int)(big >> 7), 2) - 127, 126);
+                    const float down = big >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - qe) << 23);
+                    const uint32_t r = r0 + 2u * i + up;
+                    const int other = __shfl_xor_sync(0xffffffffu, qe, 16);
+                    if ((uint32_t)lane == r) my_exp = qe;
+                    if ((uint32_t)lane == (r ^ 1u)) my_exp = other;   // (the other half warp's row of the pair)
+                    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                    uint32_t o[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const __half2 y = __floats2half2_rn(__uint_as_float(r[j] << 16) * down, __uint_as_float(r[j] & 0xFFFF0000u) * down);
-                        w[j] = *reinterpret_cast<const uint32_t *>(&y);
+                        const __half2 y = __floats2half2_rn(__uint_as_float(w[j] << 16) * down, __uint_as_float(w[j] & 0xFFFF0000u) * down);
+                        o[j] = *reinterpret_cast<const uint32_t *>(&y);
                     }
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_base + (c >> 3) * kBlock + r * 128u + (((c & 7u) ^ (r & 7u)) << 4)),
+                                 "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+                                 : "memory");
                 }
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_row + (c >> 3) * kBlock + (((c & 7u) ^ (row & 7u)) << 4)), "r"(w[0]),
-                             "r"(w[1]), "r"(w[2]), "r"(w[3])
-                             : "memory");
             }
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kBarQReady + (int)x));
-            return __uint_as_float((uint32_t)(qe + 127) << 23) * p.scale_log2;
+            return __uint_as_float((uint32_t)(my_exp + 127) << 23) * p.scale_log2;
         };
         auto has_rows = [&](const cart_shared_unit &u) { return x == 0u || u.n_readers > tpt; };   // the M-tile takes part
-        uint32_t uses = 0;       // tiles of this M-tile so far
+        uint32_t halves = 0;     // halves of tiles of this M-tile so far
         uint32_t tiles = 0;      // tiles of the block so far
         float m_run = -INFINITY, l_run = 0.f;
         bool fresh = true;       // no tile of the chain has been seen yet
@@ -620,7 +636,6 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                     on_next = i_reader < uq.n_readers;
                     head_next = uq.kv_head;
                     batch_next = on_next ? p.readers[uq.reader_begin + i_reader] : 0u;
-                    asm volatile("prefetch.global.L2 [%0];" ::"l"(q_src(head_next, batch_next)));
                 }
             }
             uint32_t slot = 0;   // where this row's partial goes, or (direct) its query row: needed at the chain's end
@@ -634,120 +649,113 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 const bool in = i_reader < (u.tr_hi & 0xFFFFu) && i_reader >= u.tr_hi >> 16;
                 limit = in && lb >= 0 ? (lb < u.lim_cap ? lb : u.lim_cap) : -1;
             }
-            for (uint32_t t = 0; t < u.n_tiles; ++t, ++uses, ++tiles) {
-                if (alive) alive = warp_wait(kBarSFull + (int)x, uses & 1u);
-                if (!alive) continue;
-                tc_fence_after();
-                const int32_t seen = limit - (int32_t)(t * (uint32_t)kTile);   // the last key of the tile this row sees
-                const uint32_t meta = base + kOffMeta + (tiles & 7u) * 128u;
-                auto meta_of = [&](int b) {
-                    float4 v;
-                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(meta + 16u * (uint32_t)b));
-                    return v;
-                };
-                // scores of keys that the row does not see (whatever stands there): -inf.  Few tiles have any; the warp decides
-                // together, so that the others pay one vote per 32.
-                auto hide = [&](uint32_t (&v)[32], int first) {
-                    if (!__any_sync(0xffffffffu, seen < first + 31)) return;
-#pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (first + k > seen) v[k] = 0xFF800000u;
-                };
-                float mx = -INFINITY;
-                uint32_t s[2][32];
-                tmem_ld32_issue(s_addr, s[0]);
+            for (uint32_t t = 0; t < u.n_tiles; ++t, ++tiles) {
 #pragma unroll 1
-                for (int c2 = 0; c2 < 4; c2 += 2)
+                for (uint32_t y = 0; y < 2; ++y, ++halves) {
+                    if (alive) alive = warp_wait(kBarSFull + (int)(2u * x + y), (halves >> 1) & 1u);
+                    if (!alive) continue;
+                    tc_fence_after();
+                    const uint32_t cols = s_addr + 64u * y;
+                    uint32_t s[2][32];
+                    tmem_ld32_issue(cols, s[0]);
+                    tmem_ld32_issue(cols + 32u, s[1]);
+                    const int32_t seen = limit - (int32_t)(t * (uint32_t)kTile + 64u * y);   // the last of the 64 keys that this row sees
+                    const uint32_t meta = base + kOffMeta + (tiles & 7u) * 128u + 64u * y;
+                    float4 mt[4];
 #pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    const int c = c2 + z;
-                    uint32_t(&v)[32] = s[z];
-                    tmem_ld_wait(v);
-                    if (z == 0 || c2 == 0) tmem_ld32_issue(s_addr + 32u * (uint32_t)(c + 1), s[z ^ 1]);
-                    hide(v, 32 * c);
+                    for (uint32_t b = 0; b < 4; ++b)
+                        asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(mt[b].x), "=f"(mt[b].y), "=f"(mt[b].z), "=f"(mt[b].w) : "r"(meta + 16u * b));
+                    tmem_ld_wait(s[0]);
+                    tmem_ld_wait(s[1]);
+                    // Scores of keys that the row does not see (whatever stands there): -inf.  Few tiles have any; the warp
+                    // decides together, so that the others pay one vote.
+                    if (__any_sync(0xffffffffu, seen < 63)) {
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const float4 mt = meta_of(2 * c + y);
-                        const uint32_t *r = v + 16 * y;
+                        for (int k = 0; k < 64; ++k)
+                            if (k > seen) s[k >> 5][k & 31] = 0xFF800000u;
+                        // (a block of which the row sees nothing may have no scale, or none at all: -inf has to stay -inf)
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+                            if (16 * b > seen) {
+                                mt[b].x = 1.f;
+                                mt[b].w = 0.f;
+                            }
+                    }
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const uint32_t *r = s[b >> 1] + 16 * (b & 1);
                         float a = max3(__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[2]));
-                        float b = max3(__uint_as_float(r[3]), __uint_as_float(r[4]), __uint_as_float(r[5]));
+                        float e = max3(__uint_as_float(r[3]), __uint_as_float(r[4]), __uint_as_float(r[5]));
                         a = max3(a, __uint_as_float(r[6]), __uint_as_float(r[7]));
-                        b = max3(b, __uint_as_float(r[8]), __uint_as_float(r[9]));
+                        e = max3(e, __uint_as_float(r[8]), __uint_as_float(r[9]));
                         a = max3(a, __uint_as_float(r[10]), __uint_as_float(r[11]));
-                        b = max3(b, __uint_as_float(r[12]), __uint_as_float(r[13]));
+                        e = max3(e, __uint_as_float(r[12]), __uint_as_float(r[13]));
                         a = max3(a, __uint_as_float(r[14]), __uint_as_float(r[15]));
                         // (a key block without a scale: a NaN, which takes no part in the maximum and stays in the sums)
-                        mx = fmaxf(mx, fmaxf(a, b) * (f_row * mt.x));
-                        if (mt.w != 0.f && 32 * c + 16 * y <= seen) marked = true;
+                        mt[b].x *= f_row;
+                        mx = fmaxf(mx, fmaxf(a, e) * mt[b].x);
+                        if (mt[b].w != 0.f) marked = true;
                     }
-                }
-                tmem_ld32_issue(s_addr, s[0]);
-                if (fresh) {
-                    m_run = mx;
-                    fresh = false;
-                } else if (__any_sync(0xffffffffu, mx > m_run + kRescaleStep)) {
-                    // a row of this warp has outgrown its reference: all of them move up and rescale.  (P V of the tile before
-                    // is complete: its product was issued before these scores', whose completion has been waited for.)
-                    const float m_new = fmaxf(m_run, mx);
-                    const float f = m_new == -INFINITY ? 1.f : fast_exp2(m_run - m_new);
-                    m_run = m_new;
-                    l_run *= f;
+                    if (fresh) {
+                        m_run = mx;
+                        fresh = false;
+                    } else if (__any_sync(0xffffffffu, mx > m_run + kRescaleStep)) {
+                        // a row of this warp has outgrown its reference: all of them move up and rescale, once P V of the half
+                        // before is complete (P V of the one before that is: these scores were issued behind it)
+                        const float m_new = fmaxf(m_run, mx);
+                        const float f = m_new == -INFINITY ? 1.f : fast_exp2(m_run - m_new);
+                        m_run = m_new;
+                        l_run *= f;
+                        alive = warp_wait(kBarOFull + (int)(2u * x + (y ^ 1u)), ((halves - 1u) >> 1) & 1u);
+                        if (!alive) continue;
+                        tc_fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        tmem_ld32_issue(o_addr + (uint32_t)c * 32u, s[1]);
-                        tmem_ld_wait(s[1]);
+                        for (uint32_t c = 0; c < 8; ++c) {
+                            uint32_t o[16];
+                            tmem_ld16(o_addr + c * 16u, o);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) s[1][k] = __float_as_uint(__uint_as_float(s[1][k]) * f);
-                        tmem_st16(o_addr + (uint32_t)c * 32u, reinterpret_cast<const uint32_t(&)[16]>(s[1][0]));
-                        tmem_st16(o_addr + (uint32_t)c * 32u + 16u, reinterpret_cast<const uint32_t(&)[16]>(s[1][16]));
-                    }
-                }
-                // probabilities times their values' scales as bf16 pairs, in the stored order of the tokens: pair 2 i of a
-                // block of 16 holds tokens 2 i and 2 i + 1, pair 2 i + 1 tokens 2 i + 8 and 2 i + 9.  (P of 32 tokens takes 16
-                // columns: it never reaches scores that have not been read.)
-                const float m_use = m_run == -INFINITY ? 0.f : m_run;
-#pragma unroll 1
-                for (int c2 = 0; c2 < 4; c2 += 2)
-#pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    const int c = c2 + z;
-                    uint32_t(&v)[32] = s[z];
-                    tmem_ld_wait(v);
-                    if (z == 0 || c2 == 0) tmem_ld32_issue(s_addr + 32u * (uint32_t)(c + 1), s[z ^ 1]);
-                    hide(v, 32 * c);
-                    uint32_t w[16];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const float4 mt = meta_of(2 * c + y);
-                        // (a block of which the row sees nothing may have no scale, or none at all: -inf stays -inf)
-                        const float cc = 32 * c + 16 * y > seen ? 1.f : f_row * mt.x, dd = mt.y - m_use;
-                        const uint64_t cc2 = pair(cc, cc), dd2 = pair(dd, dd);
-                        uint64_t sum = pair(0.f, 0.f);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int tok = 2 * (j >> 1) + 8 * (j & 1);
-                            float2 e = unpair(fma2(pair(__uint_as_float(v[16 * y + tok]), __uint_as_float(v[16 * y + tok + 1])), cc2, dd2));
-                            e.x = fast_exp2(e.x);
-                            e.y = fast_exp2(e.y);
-                            sum = add2(sum, pair(e.x, e.y));
-                            w[8 * y + j] = pack_bf16(e.x, e.y);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st16(o_addr + c * 16u, o);
                         }
-                        const float2 t2 = unpair(sum);
-                        l_run = fmaf(t2.x + t2.y, mt.z, l_run);
                     }
-                    tmem_st16(s_addr + (uint32_t)c * 16u, w);
+                    // probabilities times their values' scales as bf16 pairs, in the stored order of the tokens: pair 2 i of a
+                    // block of 16 holds tokens 2 i and 2 i + 1, pair 2 i + 1 tokens 2 i + 8 and 2 i + 9
+                    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const float cc = mt[2 * c + z].x, dd = mt[2 * c + z].y - m_use;
+                            const uint64_t cc2 = pair(cc, cc), dd2 = pair(dd, dd);
+                            uint64_t sum = pair(0.f, 0.f);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const int tok = 16 * z + 2 * (j >> 1) + 8 * (j & 1);
+                                float2 e = unpair(fma2(pair(__uint_as_float(s[c][tok]), __uint_as_float(s[c][tok + 1])), cc2, dd2));
+                                e.x = fast_exp2(e.x);
+                                e.y = fast_exp2(e.y);
+                                sum = add2(sum, pair(e.x, e.y));
+                                w[8 * z + j] = pack_bf16(e.x, e.y);
+                            }
+                            const float2 t2 = unpair(sum);
+                            l_run = fmaf(t2.x + t2.y, mt[2 * c + z].z, l_run);
+                        }
+                        tmem_st16(cols + 16u * (uint32_t)c, w);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(kBarPReady + (int)(2u * x + y)));
                 }
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kBarPReady + (int)x));
-                // the chain's query rows have been read for the last time (its last scores are here): the next one's come
-                if (!hold && t + 1u == u.n_tiles && uq_next < unit_end) f_next = bring_q(head_next, batch_next, on_next);
             }
+            // the chain's query rows have been read for the last time (its last scores have been here): the next one's come
+            if (!hold && uq_next < unit_end && alive) f_next = bring_q(head_next, batch_next, on_next);
             if (hold) continue;
 
             // ---- the chain's end: the rows leave --------------------------------------------------------------
-            if (alive) alive = warp_wait(kBarOFull + (int)x, (uses - 1u) & 1u);
+            if (alive) alive = warp_wait(kBarOFull + (int)(2u * x + 1u), ((halves - 1u) >> 1) & 1u);
             if (alive) {
                 tc_fence_after();
                 const float poison = marked ? __uint_as_float(0x7FC00000u) : 1.f;
