@@ -12,7 +12,8 @@
 //                      scales, 8-byte stores into the swizzled tiles.  The next loads are in flight meanwhile.
 //                      No raw tile is staged in shared memory: its bandwidth is what the products need (per tile and
 //                      pair of M-tiles 192 KB of operands are read and 64 KB written, as long as the products take).
-//   MMA thread         A tile's keys are dealt with in halves: S of 64 keys, its softmax, P V of these 64 tokens.  As soon as
+//   2 MMA threads      one per M-tile, of different warps (issuing the two M-tiles' 48 instructions a tile from one thread
+//                      took 1.5 times as long as executing them).  A tile's keys are dealt with in halves: S of 64 keys, its softmax, P V of these 64 tokens.  As soon as
 //                      a half's P is there, its P V is issued and behind it S of the same half of the next tile, into the
 //                      same columns; the softmax meanwhile has the other half.  So neither waits for the other's latency
 //                      (with whole tiles a row's softmax, P V and S took turns: 6000 cycles a tile, 2048 of them
@@ -51,7 +52,7 @@ constexpr uint32_t kTileBytes = 2u * kBlock;          // 128 x 128 bf16
 constexpr int kKStages = 3;
 constexpr int kVStages = 2;
 constexpr int kConvWarps = 8;
-constexpr int kThreads = 640;                         // utility warpgroup (warp 0: MMA), 2 softmax and 2 converter warpgroups
+constexpr int kThreads = 640;                         // utility warpgroup (warps 0, 1: MMA), 2 softmax and 2 converter warpgroups
 // Registers per thread after the warpgroups have re-divided the launch's 640 x 96 = 61440:
 // 128 x 56 + 256 x 136 + 256 x 72 = 60416.
 constexpr int kRegsUtility = 56;
@@ -76,16 +77,16 @@ static_assert(kSmemBytes <= 232448, "shared memory budget of one sm_100 block ex
 
 enum Bar : int {
     kBarKFull = 0,   // [kKStages] converters -> MMA (one arrival per warp)
-    kBarKEmpty = 3,  // [kKStages] MMA (commit of the tile's last score product) -> converters
+    kBarKEmpty = 3,  // [kKStages] both MMA threads (commit of the tile's last score product) -> converters
     kBarVFull = 6,   // [kVStages]
-    kBarVEmpty = 8,  // [kVStages] MMA (commit of the tile's last P V product) -> converters
+    kBarVEmpty = 8,  // [kVStages] both MMA threads (commit of the tile's last P V product) -> converters
     kBarSFull = 10,  // [M-tile][half] MMA (commit, and an arrival that passes the converters' scales on) -> softmax: the
                      // scores are there, and so is P V of the same half of the tile before
     kBarPReady = 14, // [M-tile][half] softmax -> MMA (4 arrivals: one per warp)
     kBarQReady = 18, // [M-tile] softmax -> MMA: a chain's query rows are in place (4 arrivals)
     kBarOFull = 20,  // [M-tile][half] MMA (commit of P V) -> softmax.  (A barrier per half: whoever waits for one has seen
                      // scores that were issued behind the phase before, so its parity is not ambiguous.)
-    kBarDrain = 24,  // MMA (commit) -> MMA, on the way out
+    kBarDrain = 24,  // [M-tile] MMA (commit) -> MMA, on the way out
 };
 
 // Instruction descriptors: fp32 accumulator, both operands K-major, M = 128; fp16, N = 64 (S), or bf16, N = 128 (P V).
@@ -267,11 +268,11 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
     if (threadIdx.x == 0) {
         for (int i = 0; i < kKStages; ++i) {
             mbar_init(bar(kBarKFull + i), kConvWarps);
-            mbar_init(bar(kBarKEmpty + i), 1);
+            mbar_init(bar(kBarKEmpty + i), 2);
         }
         for (int i = 0; i < kVStages; ++i) {
             mbar_init(bar(kBarVFull + i), kConvWarps);
-            mbar_init(bar(kBarVEmpty + i), 1);
+            mbar_init(bar(kBarVEmpty + i), 2);
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(bar(kBarSFull + i), 2);
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
             mbar_init(bar(kBarOFull + i), 1);
         }
         for (int i = 0; i < 2; ++i) mbar_init(bar(kBarQReady + i), 4);
-        mbar_init(bar(kBarDrain), 1);
+        for (int i = 0; i < 2; ++i) mbar_init(bar(kBarDrain + i), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -295,82 +296,84 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUtility));
-        if (warp == 0 && lane == 0) {
-            // ================= MMA issuer: one thread ========================================================
+        if (warp < 2 && lane == 0) {
+            // ================= MMA issuers: warp x's first thread for M-tile x ================================
+            const uint32_t x = (uint32_t)warp;
             bool ok = true;
             auto wait = [&](int b, uint32_t parity) -> bool {
                 return mbar_wait(bar(b), parity, abort_flag, p.status, kStatusTimeoutMma);
             };
-            // where the next score products are: unit, tile in it, tiles of the unit; the chain before it
-            uint32_t ui = unit_begin, t = 0, n = 0, two = 0, fresh = 1;
+            // where the next scores are: unit, tile in it, tiles of the unit; whether the M-tile takes part in it, whether it
+            // begins a chain
+            uint32_t ui = unit_begin, t = 0, n = 0;
+            bool mine = false, fresh = true;
             auto unit = [&]() {
                 if (ui >= unit_end) return;
                 const cart_shared_unit u = p.units[ui];
                 n = u.n_tiles;
-                two = u.n_readers > tpt ? 1u : 0u;
-                fresh = (u.flags & CART_UNIT_CONT) ? 0u : 1u;
+                mine = x == 0u || u.n_readers > tpt;
+                fresh = !(u.flags & CART_UNIT_CONT);
             };
             unit();
-            uint32_t q_uses = 0, p_uses = 0;   // bit x: parity of the chains whose rows, and of the tiles whose P, M-tile x has delivered
+            uint32_t q_par = 0, p_par = 0;   // parities: of the chains whose rows, of the tiles whose P, have been delivered
             uint32_t kst = 0, kpar = 0, vst = 0, vpar = 0;
-            // S of half y of the tile in front for M-tile x: its columns last held P, which a P V product issued earlier reads
-            auto issue_s = [&](uint32_t x, uint32_t y) {
+            const uint64_t q_desc = umma_desc(base + kOffQ + x * kTileBytes, 16, 1024);
+            // S of half y of the tile in front: its columns last held P, which a P V product issued earlier reads
+            auto issue_s = [&](uint32_t y) {
                 tc_fence_after();
-                product_s(tmem + x * 128u + y * 64u, umma_desc(base + kOffQ + x * kTileBytes, 16, 1024),
-                          umma_desc(base + kOffK + kst * kTileBytes + y * (kBlock / 2u), 16, 1024));
+                product_s(tmem + x * 128u + y * 64u, q_desc, umma_desc(base + kOffK + kst * kTileBytes + y * (kBlock / 2u), 16, 1024));
                 mma_commit(bar(kBarSFull + (int)(2u * x + y)));
                 mbar_arrive(bar(kBarSFull + (int)(2u * x + y)));
             };
-            // (Written once, for both M-tiles and halves and for the first tile too: the roles share an instruction cache.)
-            bool have = false;               // there is a current tile
-            uint32_t cur_two = 0, cur_first = 0;
+            // (Written once, for both halves and for the first tile too: the roles share an instruction cache.)
+            bool have = false, cur_mine = false, cur_first = false;   // the current tile: there is one, ...
             while (ok && (have || ui < unit_end)) {
-                const bool more = ui < unit_end;
-                const uint32_t nxt_two = two, nxt_first = (t == 0u && fresh) ? 1u : 0u;
-                if (have) ok = wait(kBarVFull + (int)vst, vpar);
-                // the current tile's P V and, in the same chain, the next tile's S
+                const bool more = ui < unit_end, nxt_mine = mine, nxt_first = t == 0u && fresh;
                 bool k_here = false;
-#pragma unroll 1
-                for (uint32_t z = 0; z < 4 && ok && have; ++z) {
-                    const uint32_t x = z & 1u, y = z >> 1;
-                    if (x == 1u && !cur_two) continue;
-                    ok = wait(kBarPReady + (int)(2u * x + y), (p_uses >> x) & 1u);
-                    if (!ok) break;
-                    tc_fence_after();
-                    product_pv(tmem + kTmemO + 128u * x, tmem + x * 128u + y * 64u, umma_desc(base + kOffV + vst * kTileBytes + y * kBlock, 16, 1024),
-                               (cur_first && y == 0u) ? 0u : 1u);
-                    mma_commit(bar(kBarOFull + (int)(2u * x + y)));
-                    if (more && !nxt_first) {
-                        if (!k_here) ok = wait(kBarKFull + (int)kst, kpar);
-                        if (!ok) break;
-                        k_here = true;
-                        issue_s(x, y);
-                    }
-                }
-                if (!ok) break;
                 if (have) {
-                    mma_commit(bar(kBarVEmpty + (int)vst));
+                    // the current tile's P V and, in the same chain, the next tile's S
+                    ok = wait(kBarVFull + (int)vst, vpar);
+#pragma unroll 1
+                    for (uint32_t y = 0; y < 2 && ok && cur_mine; ++y) {
+                        ok = wait(kBarPReady + (int)(2u * x + y), p_par);
+                        if (!ok) break;
+                        tc_fence_after();
+                        product_pv(tmem + kTmemO + 128u * x, tmem + x * 128u + y * 64u,
+                                   umma_desc(base + kOffV + vst * kTileBytes + y * kBlock, 16, 1024), (cur_first && y == 0u) ? 0u : 1u);
+                        mma_commit(bar(kBarOFull + (int)(2u * x + y)));
+                        if (more && !nxt_first) {
+                            if (!k_here) ok = wait(kBarKFull + (int)kst, kpar);
+                            if (!ok) break;
+                            k_here = true;
+                            issue_s(y);
+                        }
+                    }
+                    if (!ok) break;
+                    // (a stage is free when both M-tiles are done with it; one that takes no part says so at once)
+                    if (cur_mine) {
+                        mma_commit(bar(kBarVEmpty + (int)vst));
+                        p_par ^= 1u;
+                    } else {
+                        mbar_arrive(bar(kBarVEmpty + (int)vst));
+                    }
                     if (++vst == (uint32_t)kVStages) {
                         vst = 0;
                         vpar ^= 1u;
                     }
-                    p_uses ^= cur_two ? 3u : 1u;
                 }
                 have = more;
                 if (!more) break;
-                if (nxt_first) {   // a new chain: its rows first
-                    ok = wait(kBarKFull + (int)kst, kpar);
-#pragma unroll 1
-                    for (uint32_t x = 0; x < 1u + nxt_two && ok; ++x) {
-                        ok = wait(kBarQReady + (int)x, (q_uses >> x) & 1u);
-                        if (!ok) break;
-                        q_uses ^= 1u << x;
-                        issue_s(x, 0u);
-                        issue_s(x, 1u);
-                    }
+                if (!k_here) ok = wait(kBarKFull + (int)kst, kpar);
+                if (ok && nxt_first && nxt_mine) {   // a new chain: its rows first
+                    ok = wait(kBarQReady + (int)x, q_par);
+                    q_par ^= 1u;
                     if (!ok) break;
+                    issue_s(0u);
+                    issue_s(1u);
                 }
-                mma_commit(bar(kBarKEmpty + (int)kst));
+                if (!ok) break;
+                if (nxt_mine) mma_commit(bar(kBarKEmpty + (int)kst));
+                else mbar_arrive(bar(kBarKEmpty + (int)kst));
                 if (++kst == (uint32_t)kKStages) {
                     kst = 0;
                     kpar ^= 1u;
@@ -380,13 +383,13 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                     t = 0;
                     unit();
                 }
-                cur_two = nxt_two;
+                cur_mine = nxt_mine;
                 cur_first = nxt_first;
             }
             // products still in flight must finish before the tensor memory is given back
-            mma_commit(bar(kBarDrain));
+            mma_commit(bar(kBarDrain + (int)x));
             const uint64_t t0 = global_timer_ns();
-            while (!mbar_try_wait(bar(kBarDrain), 0) && global_timer_ns() - t0 < kWaitLimitNs) {}
+            while (!mbar_try_wait(bar(kBarDrain + (int)x), 0) && global_timer_ns() - t0 < kWaitLimitNs) {}
         }
     } else if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
