@@ -225,23 +225,23 @@ __device__ __forceinline__ uint2 to_f16(uint32_t r)
     }
     return o;
 }
-// Four stored codes -> four bf16 numbers times a power of two (a pair of bf16), exact.
+// Four stored codes -> four bf16 numbers, exact.
 template <int kFmt>
-__device__ __forceinline__ uint2 to_bf16(uint32_t r, uint32_t factor)
+__device__ __forceinline__ uint2 to_bf16(uint32_t r)
 {
     uint2 o;
     if (kFmt == CART_Q8_INT8) {
         // A byte u = code + 128 below the byte 0x43 reads, without its top bit, as the bf16 number 128 + (u mod 128); the
         // code is that less 128 if the top bit is set, less 256 if not.
         const uint32_t x = __byte_perm(r, 0x43434343u, 0x4140), y = __byte_perm(r, 0x43434343u, 0x4342);
-        o.x = bf162_mul(bf162_sub(x & 0xFF7FFF7Fu, (x & 0xFF80FF80u) ^ 0x00800080u), factor);
-        o.y = bf162_mul(bf162_sub(y & 0xFF7FFF7Fu, (y & 0xFF80FF80u) ^ 0x00800080u), factor);
+        o.x = bf162_sub(x & 0xFF7FFF7Fu, (x & 0xFF80FF80u) ^ 0x00800080u);
+        o.y = bf162_sub(y & 0xFF7FFF7Fu, (y & 0xFF80FF80u) ^ 0x00800080u);
     } else {
         // e4m3's exponent and mantissa bits, moved to the low end of bf16's exponent and the high end of its mantissa, are
         // the number times 2^-120, subnormals included.
         const uint32_t x = __byte_perm(r, 0u, 0x1404), y = __byte_perm(r, 0u, 0x3424);
-        o.x = bf162_mul(bf162_mul(((x >> 4) & 0x07F007F0u) | (x & 0x80008000u), 0x7B807B80u), factor);
-        o.y = bf162_mul(bf162_mul(((y >> 4) & 0x07F007F0u) | (y & 0x80008000u), 0x7B807B80u), factor);
+        o.x = bf162_mul(((x >> 4) & 0x07F007F0u) | (x & 0x80008000u), 0x7B807B80u);
+        o.y = bf162_mul(((y >> 4) & 0x07F007F0u) | (y & 0x80008000u), 0x7B807B80u);
     }
     return o;
 }
@@ -499,27 +499,29 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
             more = next_keys();
             ok = wait_conv(kBarVEmpty + (int)vst, vpar);
             if (!ok) break;
-            uint32_t m0 = 0xFFFFFFFFu, m1 = 0xFFFFFFFFu;   // tokens behind the end count as zeros
-            if (none) {
-                m0 = m1 = 0u;
-            } else if (cur_left < 16u) {
-                m0 = (2u * t4 < cur_left ? 0xFFFFu : 0u) | (2u * t4 + 1u < cur_left ? 0xFFFF0000u : 0u);
-                m1 = (2u * t4 + 8u < cur_left ? 0xFFFFu : 0u) | (2u * t4 + 9u < cur_left ? 0xFFFF0000u : 0u);
-            }
-            // (a scale beyond what the probabilities carry)
-            const uint32_t over = none ? 127u : (uint32_t)((int)ev - fold);
-            const uint32_t extra = over << 7 | over << 23;
             const uint32_t dst = v_at + vst * kTileBytes;
+            auto put = [&](auto edit) {
 #pragma unroll
-            for (uint32_t c = 0; c < 4; ++c) {
-                const uint32_t w[4] = {cv[c].x, cv[c].y, cv[c].z, cv[c].w};
+                for (uint32_t c = 0; c < 4; ++c) {
+                    const uint32_t w[4] = {cv[c].x, cv[c].y, cv[c].z, cv[c].w};
 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) {
-                    const uint2 v = to_bf16<kFmt>(w[j], extra);
-                    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(dst + (2u * c + (j >> 1)) * 2048u + (j & 1u) * 1024u), "r"(v.x & m0),
-                                 "r"(v.y & m1)
-                                 : "memory");
+                    for (uint32_t j = 0; j < 4; ++j) {
+                        const uint2 v = edit(to_bf16<kFmt>(w[j]));
+                        asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(dst + (2u * c + (j >> 1)) * 2048u + (j & 1u) * 1024u), "r"(v.x),
+                                     "r"(v.y)
+                                     : "memory");
+                    }
                 }
+            };
+            if (cur_left >= 16u && !none && (int)ev - 127 == fold) {
+                put([](uint2 v) { return v; });
+            } else {
+                // tokens behind the end, and a block without a scale, count as zeros; a scale beyond what the probabilities carry
+                const uint32_t over = none ? 127u : (uint32_t)((int)ev - fold), extra = over << 7 | over << 23;
+                const uint32_t end = none ? 0u : cur_left;
+                const uint32_t m0 = (2u * t4 < end ? 0xFFFFu : 0u) | (2u * t4 + 1u < end ? 0xFFFF0000u : 0u);
+                const uint32_t m1 = (2u * t4 + 8u < end ? 0xFFFFu : 0u) | (2u * t4 + 9u < end ? 0xFFFF0000u : 0u);
+                put([&](uint2 v) { return make_uint2(bf162_mul(v.x, extra) & m0, bf162_mul(v.y, extra) & m1); });
             }
             fence_async_smem();
             __syncwarp();
@@ -547,45 +549,41 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
         };
         // A chain's rows into the swizzled K-major operand -- block w (64 dims), 16-byte chunk c at position c ^ (row % 8) -- as
         // fp16 over the power of two that brings a row's largest value to 1 .. 2 (see cart_q8.cu); a row with a NaN or an
-        // infinity as NaN, rows past the readers as zeros.  The warp brings its 32 rows together, 16 lanes a row, eight rows'
-        // loads in flight.  Returns what takes the thread's own row's scores to base-2 exponents: 2^e scale log2(e).
+        // infinity as NaN, rows past the readers as zeros.  The warp brings its 32 rows together, 16 lanes a row, all loads in
+        // flight.  Returns what takes the thread's own row's scores to base-2 exponents: 2^e scale log2(e).
         const uint32_t q_base = base + kOffQ + x * kTileBytes + 32u * sw * 128u;
         auto bring_q = [&](uint32_t kv_head, uint32_t batch, bool on) -> float {
             const uint32_t c = (uint32_t)lane & 15u, up = (uint32_t)lane >> 4;
             const uint32_t from = on ? batch * (uint32_t)p.n_q_heads + kv_head * G + h : ~0u;   // the row's place among all of q's
             int my_exp = 0;
-#pragma unroll 1
-            for (uint32_t r0 = 0; r0 < 32u; r0 += 8u) {
-                uint4 v[4];
+            uint4 v[16];
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t src = __shfl_sync(0xffffffffu, from, (int)(r0 + 2u * i + up));
-                    v[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (src != ~0u) v[i] = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) + (size_t)src * kHeadDim) + c);
+            for (uint32_t i = 0; i < 16; ++i) {
+                const uint32_t src = __shfl_sync(0xffffffffu, from, (int)(2u * i + up));
+                v[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (src != ~0u) v[i] = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) + (size_t)src * kHeadDim) + c);
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) {
+                uint32_t big = __vmaxu2(__vmaxu2(v[i].x & 0x7FFF7FFFu, v[i].y & 0x7FFF7FFFu), __vmaxu2(v[i].z & 0x7FFF7FFFu, v[i].w & 0x7FFF7FFFu));
+                big = max(big & 0xFFFFu, big >> 16);
+                big = __reduce_max_sync(0xFFFFu << (16u * up), big);
+                const int qe = big >= 0x7F80u ? 0 : min(max((int)(big >> 7), 2) - 127, 126);
+                const float down = big >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - qe) << 23);
+                const uint32_t r = 2u * i + up;
+                const int other = __shfl_xor_sync(0xffffffffu, qe, 16);
+                if ((uint32_t)lane == r) my_exp = qe;
+                if ((uint32_t)lane == (r ^ 1u)) my_exp = other;   // (the other half warp's row of the pair)
+                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                uint32_t o[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const __half2 y = __floats2half2_rn(__uint_as_float(w[j] << 16) * down, __uint_as_float(w[j] & 0xFFFF0000u) * down);
+                    o[j] = *reinterpret_cast<const uint32_t *>(&y);
                 }
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    uint32_t big = __vmaxu2(__vmaxu2(v[i].x & 0x7FFF7FFFu, v[i].y & 0x7FFF7FFFu), __vmaxu2(v[i].z & 0x7FFF7FFFu, v[i].w & 0x7FFF7FFFu));
-                    big = max(big & 0xFFFFu, big >> 16);
-#pragma unroll
-                    for (int d = 1; d < 16; d <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
-                    const int qe = big >= 0x7F80u ? 0 : min(max((int)(big >> 7), 2) - 127, 126);
-                    const float down = big >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - qe) << 23);
-                    const uint32_t r = r0 + 2u * i + up;
-                    const int other = __shfl_xor_sync(0xffffffffu, qe, 16);
-                    if ((uint32_t)lane == r) my_exp = qe;
-                    if ((uint32_t)lane == (r ^ 1u)) my_exp = other;   // (the other half warp's row of the pair)
-                    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                    uint32_t o[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const __half2 y = __floats2half2_rn(__uint_as_float(w[j] << 16) * down, __uint_as_float(w[j] & 0xFFFF0000u) * down);
-                        o[j] = *reinterpret_cast<const uint32_t *>(&y);
-                    }
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_base + (c >> 3) * kBlock + r * 128u + (((c & 7u) ^ (r & 7u)) << 4)),
-                                 "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
-                                 : "memory");
-                }
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_base + (c >> 3) * kBlock + r * 128u + (((c & 7u) ^ (r & 7u)) << 4)),
+                             "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+                             : "memory");
             }
             fence_async_smem();
             __syncwarp();
