@@ -33,7 +33,7 @@ Q8Layout q8_layout(const cart_config &c)
     // as for the bf16 plans: a row group owns at most parts + 2 segments, a block boundary cuts an item in two
     s.items_cap = row_groups * (parts + 2) + kQ8MaxCta;
     s.merges_cap = row_groups + kQ8MaxCta;
-    s.slots_cap = 10 * row_groups + 2 * kQ8MaxCta;
+    s.slots_cap = (std::max(parts, 8) + 4) * row_groups + 4 * kQ8MaxCta;  // a piece per part and row group at least, and the cuts
     s.readers_cap = c.max_requests * (parts + 1);
     s.units_cap = s.readers_cap * c.n_kv_heads + kQ8MaxCta;
     s.pages_cap = 256 * c.max_requests + 65536;  // 16 k tokens a request on average, and 4 M tokens besides
@@ -85,13 +85,15 @@ struct Slot {
     // a plan's tables (offsets into the slot); the page list comes first
     uint64_t cta_off = 0, items_off = 0, merges_off = 0;
     int32_t n_items = 0, n_merges = 0, n_cta_used = 0;
-    struct Tiles { uint64_t cta_off = 0, units_off = 0, readers_off = 0, slots_off = 0; int32_t n_cta = 0; } tiles[2];  // shared parts; messages
+    uint64_t unit_cta_off = 0, units_off = 0, readers_off = 0, slots_off = 0;   // the tcgen05 kernel's
+    int32_t n_unit_cta = 0;
 };
 
 // Work for the tcgen05 kernel, as its tables want it.
 struct TileWork {
     std::vector<cart_shared_unit> units;
     std::vector<uint32_t> cta, readers, slots;  // units before block c; query row per reader; first slot per (reader, KV head)
+    uint32_t n_heads = 0;
 };
 
 }  // namespace
@@ -107,8 +109,8 @@ struct Q8State {
     std::vector<cart_plan_seg> seg_tmp;
     std::vector<cart_work_item> item_tmp;
     std::vector<cart_merge_item> merge_tmp;
-    std::vector<uint32_t> cta_tmp, row_tmp;
-    TileWork work_tmp[2];
+    std::vector<uint32_t> cta_tmp, row_tmp, count_tmp;
+    TileWork work_tmp;
 };
 
 void q8_release(Q8State *st)
@@ -387,21 +389,54 @@ constexpr int kStreamPieceTiles = 1;
 // What a chain's piece costs a block beside its tiles (its rows fetched, its result written), in tile times.
 constexpr uint32_t kPieceTiles = 3;
 
-// Messages as chains of units (cart_plan.h): rows of messages that stand behind the same parts are packed into M-tiles
-// of 128 / G; a chain is an M-tile times a KV head, over the parts' tiles, then message by message the tiles of the
-// tokens that its rows see, masked causally.  All chains laid end to end are cut into equal shares, one per block.  A
-// chain in one piece writes its rows itself; the pieces of a cut one leave partials for the merge kernel.  Returns the
-// number of blocks.
-int32_t plan_messages(const Q8State *st, const CtxView &cv, int32_t layer, std::vector<Message> &messages, int n_cta, int32_t slots_cap,
-                      int32_t *n_slots, std::vector<cart_merge_item> *merges, TileWork *w)
+// A part that this many rows of the stream or more name is worth a tcgen05 launch when together the rows would stream this
+// many tokens (times KV heads) of shared parts: the stream kernel does about 25 a nanosecond out of L2, and the launch, its
+// first tile and the merge that then is needed take some 20 us (128 rows over 4096 tokens: 70 us against 169 streamed; 8 rows
+// over 2048: 30 against 15).
+constexpr int64_t kShareTokens = 600000;
+constexpr int32_t kShareMinLen = 64;   // a shorter part is half of a tile at most
+
+// The tcgen05 kernel's work (cart_plan.h): rows of messages that stand behind the same parts, and rows that share a part, are
+// packed into units of two M-tiles, 2 * (128 / G) rows; a chain is a unit's rows times a KV head over its runs: a shared part's
+// tiles, or the parts' tiles and then, message by message, the tiles of the tokens that its rows see, masked causally.
+struct TilePlan {
+    struct Rows { uint32_t reader_begin, n_readers, first_run, n_runs, n_tiles; };
+    std::vector<Rows> rows;
+    std::vector<cart_shared_unit> runs;     // without their KV head
+    struct Piece { uint32_t rows, head, t0, t1; };
+    std::vector<Piece> pieces;              // of the chains, in order: rows, then KV heads
+    std::vector<uint32_t> first;            // pieces before block c
+};
+
+constexpr uint32_t kTileTok = (uint32_t)kShareTileTokens;
+
+void add_run(TilePlan *tp, uint32_t Hkv, uint32_t list_base, uint32_t n_tok, int32_t lim_base, uint32_t tr_lo, uint32_t tr_hi, uint32_t flags)
 {
-    const uint32_t Hkv = (uint32_t)cv.cfg->n_kv_heads, tpt = 2u * (128u / (uint32_t)cv.group);   // two M-tiles
+    TilePlan::Rows &t = tp->rows.back();
+    cart_shared_unit u{};
+    u.k_row = list_base;
+    u.layer_stride = Hkv;
+    u.n_tiles = (n_tok + kTileTok - 1) / kTileTok;
+    u.reader_begin = t.reader_begin;
+    u.n_readers = t.n_readers;
+    u.flags = (uint16_t)(CART_UNIT_PAGED | flags);
+    u.lim_base = lim_base;
+    u.lim_cap = (int32_t)n_tok - 1;
+    u.tr_hi = tr_lo << 16 | tr_hi;
+    tp->runs.push_back(u);
+    ++t.n_runs;
+    t.n_tiles += u.n_tiles;
+}
+// A part, which every row sees whole (a ragged end is masked as the end of the run).
+void add_part(TilePlan *tp, uint32_t Hkv, const Cache &c, int32_t n)
+{
+    add_run(tp, Hkv, c.list_base, (uint32_t)n, n - 1, 0u, 0xFFFFu, (uint32_t)n % kTileTok ? CART_UNIT_MASKED : 0u);
+}
+
+void add_messages(TilePlan *tp, const Q8State *st, const CtxView &cv, int32_t layer, std::vector<Message> &messages, TileWork *w)
+{
+    const uint32_t Hkv = (uint32_t)cv.cfg->n_kv_heads, upt = 2u * (128u / (uint32_t)cv.group);
     std::stable_sort(messages.begin(), messages.end(), [](const Message &a, const Message &b) { return a.c->parts < b.c->parts; });
-    // the runs of every M-tile (the same for all KV heads): units without their KV head, and how many tiles they have
-    struct Tile { uint32_t reader_begin, n_readers, first_run, n_runs, n_tiles; };
-    std::vector<Tile> m_tiles;
-    std::vector<cart_shared_unit> runs;
-    constexpr uint32_t T = (uint32_t)kShareTileTokens;
     for (size_t a = 0; a < messages.size();) {
         size_t b = a;
         uint32_t rows = 0;
@@ -409,143 +444,175 @@ int32_t plan_messages(const Q8State *st, const CtxView &cv, int32_t layer, std::
         const uint32_t reader0 = (uint32_t)w->readers.size();
         for (size_t x = a; x < b; ++x)
             for (int32_t r = 0; r < messages[x].n_rows; ++r) w->readers.push_back(messages[x].row0 + (uint32_t)r);
-        for (uint32_t r0 = 0; r0 < rows; r0 += tpt) {
-            Tile t{reader0 + r0, std::min(tpt, rows - r0), (uint32_t)runs.size(), 0u, 0u};
-            auto add = [&](uint32_t list_base, uint32_t n_tok, int32_t lim_base, uint32_t tr_lo, uint32_t tr_hi, uint32_t flags) {
-                cart_shared_unit u{};
-                u.k_row = list_base;
-                u.layer_stride = Hkv;
-                u.n_tiles = (n_tok + T - 1) / T;
-                u.reader_begin = t.reader_begin;
-                u.n_readers = t.n_readers;
-                u.flags = (uint16_t)(CART_UNIT_PAGED | flags);
-                u.lim_base = lim_base;
-                u.lim_cap = (int32_t)n_tok - 1;
-                u.tr_hi = tr_lo << 16 | tr_hi;
-                runs.push_back(u);
-                ++t.n_runs;
-                t.n_tiles += u.n_tiles;
-            };
+        for (uint32_t r0 = 0; r0 < rows; r0 += upt) {
+            const uint32_t n = std::min(upt, rows - r0);
+            tp->rows.push_back(TilePlan::Rows{reader0 + r0, n, (uint32_t)tp->runs.size(), 0u, 0u});
             for (int32_t q : messages[a].c->parts) {
                 const Cache &c = st->caches[(size_t)q];
-                const int32_t n = c.len[(size_t)layer];
-                // (every row sees all of it; a ragged end is masked as the end of the run)
-                if (n > 0) add(c.list_base, (uint32_t)n, n - 1, 0u, 0xFFFFu, (uint32_t)n % T ? CART_UNIT_MASKED : 0u);
+                if (c.len[(size_t)layer] > 0) add_part(tp, Hkv, c, c.len[(size_t)layer]);
             }
             uint32_t at = 0;   // first row of message x among the pack's
             for (size_t x = a; x < b; at += (uint32_t)messages[x].n_rows, ++x) {
                 const Message &m = messages[x];
-                const uint32_t lo = std::max(at, r0), hi = std::min(at + (uint32_t)m.n_rows, r0 + t.n_readers);
+                const uint32_t lo = std::max(at, r0), hi = std::min(at + (uint32_t)m.n_rows, r0 + n);
                 if (lo >= hi) continue;
                 const int32_t key0 = m.len - m.n_rows;   // row r of the message sees its tokens 0 .. key0 + r
-                add(m.c->list_base, (uint32_t)(key0 + (int32_t)(hi - 1 - at) + 1), key0 + (int32_t)r0 - (int32_t)at, lo - r0, hi - r0,
-                    CART_UNIT_MASKED | CART_UNIT_SUFFIX);
+                add_run(tp, Hkv, m.c->list_base, (uint32_t)(key0 + (int32_t)(hi - 1 - at) + 1), key0 + (int32_t)r0 - (int32_t)at, lo - r0,
+                        hi - r0, CART_UNIT_MASKED | CART_UNIT_SUFFIX);
             }
-            m_tiles.push_back(t);
         }
         a = b;
     }
-    uint64_t W = 0;
-    for (const Tile &t : m_tiles) W += (uint64_t)t.n_tiles * Hkv;
-    const uint64_t n_chains = (uint64_t)m_tiles.size() * Hkv;
-    w->slots.assign(w->readers.size() * Hkv, 0u);
-    struct Piece { uint32_t tile, head, t0, t1; };
-    std::vector<Piece> pieces;
-    std::vector<uint32_t> first;   // pieces before block c
-    uint64_t C = std::min<uint64_t>((uint64_t)n_cta, std::max<uint64_t>(1, W / 2));
-    for (;; C = (C + 1) / 2) {
-        pieces.clear();
-        first.assign(1, 0u);
-        uint64_t tiles_left = W, chains_left = n_chains, budget = 0, acc = 0, c = 0;
-        auto open = [&](bool mid) {   // an equal share of the weight that is left, counting a cut for every block still to come
-            const uint64_t blocks = C - c;
-            budget = (tiles_left + kPieceTiles * (chains_left + (mid ? 1 : 0) + (blocks - 1)) + blocks - 1) / blocks;
-            acc = 0;
-        };
-        open(false);
-        int64_t need = 0;
-        for (size_t i = 0; i < m_tiles.size(); ++i)
-            for (uint32_t h = 0; h < Hkv; ++h) {
-                const uint32_t n = m_tiles[i].n_tiles;
-                uint32_t done = 0, cut = 0;
-                while (done < n) {
-                    uint32_t take = n - done;
-                    if (c + 1 < C) {
-                        const uint64_t room = budget > acc + kPieceTiles ? budget - acc - kPieceTiles : 0;
-                        if (room < 2 && acc > 0) {   // too little left for a piece
-                            first.push_back((uint32_t)pieces.size());
-                            ++c;
-                            open(done > 0);
-                            continue;
-                        }
-                        // (no piece of less than two tiles is left behind)
-                        if (take > room) take = (uint32_t)std::max<uint64_t>(room, 2);
-                        if (n - done - std::min(take, n - done) < 2) take = n - done;
+}
+
+// Cuts the chains, laid end to end, into at most C equal shares, one per block: a tile weighs 1, a piece kPieceTiles more.
+void cut_chains(TilePlan *tp, uint32_t Hkv, uint64_t C)
+{
+    uint64_t tiles_left = 0, chains_left = (uint64_t)tp->rows.size() * Hkv, budget = 0, acc = 0, c = 0;
+    for (const auto &t : tp->rows) tiles_left += (uint64_t)t.n_tiles * Hkv;
+    C = std::min<uint64_t>(C, std::max<uint64_t>(1, tiles_left / 2));
+    tp->pieces.clear();
+    tp->first.assign(1, 0u);
+    auto open = [&](bool mid) {   // an equal share of the weight that is left, counting a cut for every block still to come
+        const uint64_t blocks = C - c;
+        budget = (tiles_left + kPieceTiles * (chains_left + (mid ? 1 : 0) + (blocks - 1)) + blocks - 1) / blocks;
+        acc = 0;
+    };
+    open(false);
+    for (size_t i = 0; i < tp->rows.size(); ++i)
+        for (uint32_t h = 0; h < Hkv; ++h) {
+            const uint32_t n = tp->rows[i].n_tiles;
+            for (uint32_t done = 0; done < n;) {
+                uint32_t take = n - done;
+                if (c + 1 < C) {
+                    const uint64_t room = budget > acc + kPieceTiles ? budget - acc - kPieceTiles : 0;
+                    if (room < 2 && acc > 0) {   // too little left for a piece
+                        tp->first.push_back((uint32_t)tp->pieces.size());
+                        ++c;
+                        open(done > 0);
+                        continue;
                     }
-                    pieces.push_back(Piece{(uint32_t)i, h, done, done + take});
-                    acc += take + kPieceTiles;
-                    tiles_left -= take;
-                    if (done == 0) --chains_left;
-                    done += take;
-                    ++cut;
+                    if (take > room) take = (uint32_t)std::min<uint64_t>(take, std::max<uint64_t>(room, 2));
+                    if (n - done - take < 2) take = n - done;   // (no piece of less than two tiles is left behind)
                 }
-                if (cut > 1) need += (int64_t)cut * m_tiles[i].n_readers;
+                tp->pieces.push_back(TilePlan::Piece{(uint32_t)i, h, done, done + take});
+                acc += take + kPieceTiles;
+                tiles_left -= take;
+                if (done == 0) --chains_left;
+                done += take;
             }
-        first.push_back((uint32_t)pieces.size());
-        if (need + *n_slots <= slots_cap || C == 1) break;
+        }
+    tp->first.push_back((uint32_t)tp->pieces.size());
+}
+
+// Partial slots and merge items of all row groups.  A row group that one piece holds whole is written by that piece; the others'
+// pieces -- of chains, then of the stream -- get consecutive slots and a merge item.  False: the slots do not suffice.
+bool place_partials(const TilePlan &tp, uint32_t Hkv, uint32_t n_rows, std::vector<cart_work_item> &items, int32_t slots_cap,
+                    std::vector<cart_merge_item> *merges, TileWork *w, std::vector<uint32_t> *count)
+{
+    std::vector<uint32_t> &n = *count;
+    n.assign((size_t)n_rows * Hkv, 0u);
+    for (const auto &pc : tp.pieces)
+        for (uint32_t r = 0; r < tp.rows[pc.rows].n_readers; ++r) ++n[(size_t)w->readers[tp.rows[pc.rows].reader_begin + r] * Hkv + pc.head];
+    for (const cart_work_item &it : items)
+        if (it.flags & CART_ITEM_END) ++n[it.row_group];
+    // A unit's rows are alike: all of them are written by it, or all leave partials.  So where some row of an uncut chain has
+    // other pieces too, the rows that have none get a slot all the same.
+    std::vector<uint8_t> wanted(n.size(), 0);
+    for (size_t rg = 0; rg < n.size(); ++rg) wanted[rg] = n[rg] > 1;
+    for (const auto &pc : tp.pieces) {
+        const auto &t = tp.rows[pc.rows];
+        bool any = false;
+        for (uint32_t r = 0; r < t.n_readers; ++r) any = any || n[(size_t)w->readers[t.reader_begin + r] * Hkv + pc.head] > 1;
+        for (uint32_t r = 0; any && r < t.n_readers; ++r) wanted[(size_t)w->readers[t.reader_begin + r] * Hkv + pc.head] = 1;
     }
-    // units, slots and merge items, piece by piece
+    uint64_t total = 0;
+    for (size_t rg = 0; rg < n.size(); ++rg) total += wanted[rg] ? n[rg] : 0;
+    if (total > (uint64_t)slots_cap) return false;
+    // from here on n[rg] is the next slot of the row group, or ~0 for one without
+    merges->clear();
+    uint32_t at = 0;
+    std::vector<uint32_t> item_of(n.size(), 0u);
+    for (size_t rg = 0; rg < n.size(); ++rg) {
+        const uint32_t k = n[rg];
+        n[rg] = ~0u;
+        if (!wanted[rg]) continue;
+        item_of[rg] = (uint32_t)merges->size();
+        merges->push_back(cart_merge_item{(uint32_t)rg, at, at + k, 0u});
+        n[rg] = at;
+        at += k;
+    }
+    // the pieces of a chain have consecutive slots per reader: piece `chunk` goes to slot + chunk
+    w->slots.assign(w->readers.size() * Hkv, 0u);
+    for (size_t x = 0; x < tp.pieces.size(); ++x) {
+        const auto &pc = tp.pieces[x];
+        if (pc.t0 > 0) continue;
+        const auto &t = tp.rows[pc.rows];
+        uint32_t k = 1;
+        while (x + k < tp.pieces.size() && tp.pieces[x + k].t0 > 0) ++k;
+        for (uint32_t r = 0; r < t.n_readers; ++r) {
+            const uint32_t e = t.reader_begin + r;
+            uint32_t &next = n[(size_t)w->readers[e] * Hkv + pc.head];
+            w->slots[(size_t)e * Hkv + pc.head] = next;
+            if (next != ~0u) next += k;
+        }
+    }
+    for (cart_work_item &it : items) {
+        if (!(it.flags & CART_ITEM_END)) continue;
+        uint32_t &next = n[it.row_group];
+        if (next == ~0u) {
+            it.flags |= CART_ITEM_DIRECT;
+        } else {
+            it.flags &= ~CART_ITEM_DIRECT;
+            it.slot = next++;
+            it.merge = item_of[it.row_group];
+        }
+    }
+    return true;
+}
+
+// The units of all pieces, block by block.
+void emit_units(const TilePlan &tp, TileWork *w)
+{
     w->cta.assign(1, 0u);
-    size_t block_end = 1;
+    w->units.clear();
+    size_t block = 1;
     uint32_t chunk = 0;
-    for (size_t x = 0; x < pieces.size(); ++x) {
-        while (x == first[block_end]) {
+    for (size_t x = 0; x < tp.pieces.size(); ++x) {
+        while (x == tp.first[block]) {
             w->cta.push_back((uint32_t)w->units.size());
-            ++block_end;
+            ++block;
         }
-        const Piece &pc = pieces[x];
-        const Tile &t = m_tiles[pc.tile];
-        const bool whole = pc.t0 == 0 && pc.t1 == t.n_tiles;
+        const auto &pc = tp.pieces[x];
+        const auto &t = tp.rows[pc.rows];
         chunk = pc.t0 == 0 ? 0u : chunk + 1u;
-        if (pc.t0 == 0 && !whole) {
-            uint32_t n = 1;
-            for (size_t y = x + 1; y < pieces.size() && pieces[y].t0 > 0; ++y) ++n;
-            for (uint32_t r = 0; r < t.n_readers; ++r) {
-                const uint32_t e = t.reader_begin + r;
-                w->slots[(size_t)e * Hkv + pc.head] = (uint32_t)*n_slots;
-                merges->push_back(cart_merge_item{w->readers[e] * Hkv + pc.head, (uint32_t)*n_slots, (uint32_t)*n_slots + n, 0u});
-                *n_slots += (int32_t)n;
-            }
-        }
+        // the piece writes its rows' output itself if they have no other piece (a unit's rows are alike in this: all of them have
+        // a place among the partials, or none has)
+        const bool direct = pc.t0 == 0 && pc.t1 == t.n_tiles && w->slots[(size_t)t.reader_begin * w->n_heads + pc.head] == ~0u;
         const size_t unit0 = w->units.size();
         uint32_t at = 0;
         for (uint32_t y = 0; y < t.n_runs; ++y) {
-            const cart_shared_unit &run = runs[t.first_run + y];
+            const cart_shared_unit &run = tp.runs[t.first_run + y];
             const uint32_t lo = std::max(at, pc.t0), hi = std::min(at + run.n_tiles, pc.t1);
             if (lo < hi) {
                 cart_shared_unit u = run;
                 const uint32_t off = lo - at;
-                u.k_row += off * (T / (uint32_t)kTileTokens);
+                u.k_row += off * (kTileTok / (uint32_t)kTileTokens);
                 u.n_tiles = hi - lo;
                 u.v_row = pc.head;
                 u.kv_head = (uint16_t)pc.head;
-                u.lim_base -= (int32_t)(off * T);
-                u.lim_cap -= (int32_t)(off * T);
+                u.lim_base -= (int32_t)(off * kTileTok);
+                u.lim_cap -= (int32_t)(off * kTileTok);
                 u.chunk = chunk;
                 u.flags |= (uint16_t)(CART_UNIT_HOLD | (w->units.size() > unit0 ? CART_UNIT_CONT : 0u));
-                // (an inner piece of a run with a ragged end does not reach that end)
                 w->units.push_back(u);
             }
             at += run.n_tiles;
         }
         w->units[unit0].reserved = (uint32_t)(w->units.size() - unit0);
-        w->units.back().flags = (uint16_t)((w->units.back().flags & ~CART_UNIT_HOLD) | (whole ? CART_UNIT_DIRECT : 0u));
+        w->units.back().flags = (uint16_t)((w->units.back().flags & ~CART_UNIT_HOLD) | (direct ? CART_UNIT_DIRECT : 0u));
     }
-    while (block_end < first.size()) {
-        w->cta.push_back((uint32_t)w->units.size());
-        ++block_end;
-    }
-    return (int32_t)w->cta.size() - 1;
+    for (; block < tp.first.size(); ++block) w->cta.push_back((uint32_t)w->units.size());
 }
 
 // Finds or makes the plan of an attention call.  n_new = null: one query per cache.
@@ -601,10 +668,61 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
     auto &segs = st->seg_tmp;
     auto &sb = st->seg_begin_tmp;
     auto &row_of = st->row_tmp;   // query row of the stream's i-th row
+    auto &items = st->item_tmp;
+    auto &merges = st->merge_tmp;
+    auto &cta = st->cta_tmp;
+    TileWork &w = st->work_tmp;
+    w.units.clear();
+    w.cta.clear();
+    w.readers.clear();
+    w.slots.clear();
+    w.n_heads = (uint32_t)Hkv;
+    items.clear();
+    merges.clear();
+    cta.clear();
     segs.clear();
     sb.assign(1, 0);
     row_of.clear();
+    const int n_cta = std::min(cv.n_cta, kQ8MaxCta);
+    const uint32_t upt = 2u * (128u / (uint32_t)cv.group);
+    TilePlan tp;
     std::vector<Message> messages;
+    // which parts the streaming rows have in common
+    std::vector<std::pair<int32_t, std::vector<uint32_t>>> shared;   // part, its readers (query rows), in order of appearance
+    std::vector<int32_t> shared_at(st->caches.size(), -1);
+    uint32_t n_rows = 0;
+    if (cv.share_min_readers > 0) {
+        for (int32_t i = 0; i < n_ids; ++i) {
+            const int32_t m = n_new ? n_new[i] : 1;
+            if (m < kChainRows)
+                for (int32_t r2 = 0; r2 < m; ++r2)
+                    for (int32_t q : st->caches[(size_t)ids[i]].parts) {
+                        if (st->caches[(size_t)q].len[(size_t)layer] < kShareMinLen) continue;
+                        if (shared_at[(size_t)q] < 0) {
+                            shared_at[(size_t)q] = (int32_t)shared.size();
+                            shared.emplace_back(q, std::vector<uint32_t>());
+                        }
+                        shared[(size_t)shared_at[(size_t)q]].second.push_back(n_rows + (uint32_t)r2);
+                    }
+            n_rows += (uint32_t)m;
+        }
+        int64_t tokens = 0;
+        for (const auto &x : shared)
+            if ((int64_t)x.second.size() >= cv.share_min_readers)
+                tokens += (int64_t)x.second.size() * st->caches[(size_t)x.first].len[(size_t)layer] * Hkv;
+        for (const auto &x : shared) {
+            if ((int64_t)x.second.size() >= cv.share_min_readers && tokens >= kShareTokens) {
+                const uint32_t reader0 = (uint32_t)w.readers.size();
+                w.readers.insert(w.readers.end(), x.second.begin(), x.second.end());
+                for (uint32_t r0 = 0; r0 < x.second.size(); r0 += upt) {
+                    tp.rows.push_back(TilePlan::Rows{reader0 + r0, std::min(upt, (uint32_t)x.second.size() - r0), (uint32_t)tp.runs.size(), 0u, 0u});
+                    add_part(&tp, (uint32_t)Hkv, st->caches[(size_t)x.first], st->caches[(size_t)x.first].len[(size_t)layer]);
+                }
+            } else {
+                shared_at[(size_t)x.first] = -1;
+            }
+        }
+    }
     auto push = [&](const Cache &c, int32_t n_tok, uint32_t flags) {
         if (n_tok <= 0) return;
         cart_plan_seg sg;
@@ -616,7 +734,7 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
         sg.flags = flags | CART_SEG_PAGED;
         segs.push_back(sg);
     };
-    uint32_t n_rows = 0;
+    n_rows = 0;
     for (int32_t i = 0; i < n_ids; ++i) {
         const Cache &c = st->caches[(size_t)ids[i]];
         const int32_t m = n_new ? n_new[i] : 1, len = c.len[(size_t)layer];
@@ -625,78 +743,50 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
             n_rows += (uint32_t)m;
             continue;
         }
-        for (int32_t r2 = 0; r2 < m; ++r2) {
-            for (int32_t q : c.parts) push(st->caches[(size_t)q], st->caches[(size_t)q].len[(size_t)layer], 0);
+        for (int32_t r2 = 0; r2 < m; ++r2, ++n_rows) {
+            for (int32_t q : c.parts)
+                if (shared_at[(size_t)q] < 0) push(st->caches[(size_t)q], st->caches[(size_t)q].len[(size_t)layer], 0);
             push(c, len - (m - 1 - r2), CART_SEG_SUFFIX);
+            if ((int32_t)segs.size() == sb.back()) continue;   // (all of it is in shared parts)
             sb.push_back((int32_t)segs.size());
-            row_of.push_back(n_rows++);
+            row_of.push_back(n_rows);
         }
     }
-    auto &items = st->item_tmp;
-    auto &merges = st->merge_tmp;
-    auto &cta = st->cta_tmp;
-    const int n_cta = std::min(cv.n_cta, kQ8MaxCta);
-    for (TileWork &w : st->work_tmp) {
-        w.units.clear();
-        w.cta.clear();
-        w.readers.clear();
-        w.slots.clear();
-    }
-    items.clear();
-    merges.clear();
-    cta.clear();
-    int32_t n_slots = 0;
+    add_messages(&tp, st, cv, layer, messages, &w);
     sl->n_cta_used = 0;
-    for (auto &t : sl->tiles) t.n_cta = 0;
+    sl->n_unit_cta = 0;
     if (!row_of.empty()) {
-        TileWork &w = st->work_tmp[0];
-        // (as much as these rows can need)
-        const size_t n_rg = row_of.size() * (size_t)Hkv, n_run = segs.size() * (size_t)Hkv;
+        const size_t n_run = segs.size() * (size_t)Hkv;   // (as much as these rows can need)
         items.resize(2 * n_run + (size_t)n_cta + 8);
-        merges.resize(n_rg + (size_t)n_cta);
+        merges.resize(row_of.size() * (size_t)Hkv + (size_t)n_cta);
         cta.resize((size_t)n_cta + 1);
-        w.units.resize(n_run + (size_t)n_cta);
-        w.cta.resize((size_t)n_cta + 1);
-        w.readers.resize(segs.size());
-        w.slots.resize(n_run);
-        std::vector<uint32_t> unused(n_run);  // merge item per (reader, KV head)
         cart_plan_out po{};
         po.items = items.data();
         po.items_cap = (int32_t)items.size();
         po.cta_begin = cta.data();
         po.merges = merges.data();
         po.merges_cap = (int32_t)merges.size();
-        po.slots_cap = lay.slots_cap;
+        po.slots_cap = INT32_MAX;
         po.piece_cost = kStreamPieceTiles;
-        po.unit_cost = cv.unit_cost;
-        po.units = w.units.data();
-        po.units_cap = (int32_t)w.units.size();
-        po.unit_cta_begin = w.cta.data();
-        po.readers = w.readers.data();
-        po.readers_cap = (int32_t)segs.size();
-        po.reader_slot = w.slots.data();
-        po.reader_merge = unused.data();
-        r = cart_plan_build_shared(segs.data(), sb.data(), (int32_t)row_of.size(), Hkv, cv.group, n_cta, kTileTokens,
-                                   cv.share_min_readers, kShareTileTokens, &po);
+        r = cart_plan_build_shared(segs.data(), sb.data(), (int32_t)row_of.size(), Hkv, cv.group, n_cta, kTileTokens, 0, kShareTileTokens, &po);
         if (r != CART_OK) return ctx_fail(ctx, r, "q8 attention: planning failed (%s)", cart_status_string(r));
         items.resize((size_t)po.n_items);
-        merges.resize((size_t)po.n_merges);
-        n_slots = po.n_slots;
         sl->n_cta_used = po.n_items > 0 ? po.n_cta_used : 0;
-        w.units.resize((size_t)po.n_units);
-        w.readers.resize((size_t)po.n_readers);
-        w.slots.resize((size_t)po.n_readers * (size_t)Hkv);
-        w.cta.resize((size_t)po.n_unit_cta_used + 1);
-        sl->tiles[0].n_cta = po.n_units > 0 ? po.n_unit_cta_used : 0;
-        for (cart_shared_unit &u : w.units) u.reserved = 1;  // every unit brings its own rows
         // the planner numbers the rows that it was given; here they have places among all rows
-        auto place = [&](uint32_t rg) { return row_of[rg / (uint32_t)Hkv] * (uint32_t)Hkv + rg % (uint32_t)Hkv; };
-        for (cart_work_item &it : items) it.row_group = place(it.row_group);
-        for (cart_merge_item &mi : merges) mi.row_group = place(mi.row_group);
-        for (uint32_t &x : w.readers) x = row_of[x];
+        for (cart_work_item &it : items)
+            it.row_group = row_of[it.row_group / (uint32_t)Hkv] * (uint32_t)Hkv + it.row_group % (uint32_t)Hkv;
     }
-    if (!messages.empty()) {
-        sl->tiles[1].n_cta = plan_messages(st, cv, layer, messages, n_cta, lay.slots_cap, &n_slots, &merges, &st->work_tmp[1]);
+    // fewer blocks, and so fewer cuts, if the partial slots do not suffice
+    bool placed = false;
+    for (uint64_t C = (uint64_t)n_cta;; C = (C + 1) / 2) {
+        if (!tp.rows.empty()) cut_chains(&tp, (uint32_t)Hkv, C);
+        placed = place_partials(tp, (uint32_t)Hkv, n_rows, items, lay.slots_cap, &merges, &w, &st->count_tmp);
+        if (placed || C == 1 || tp.rows.empty()) break;
+    }
+    if (!placed) return ctx_fail(ctx, CART_ERR_CAPACITY, "q8 attention: the batch needs more than %d partial slots", lay.slots_cap);
+    if (!tp.rows.empty()) {
+        emit_units(tp, &w);
+        sl->n_unit_cta = (int32_t)w.cta.size() - 1;
     }
     sl->n_items = (int32_t)items.size();
     sl->n_merges = (int32_t)merges.size();
@@ -714,13 +804,11 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
     sl->cta_off = put(cta.data(), cta.size() * 4);
     sl->items_off = put(items.data(), items.size() * sizeof(cart_work_item));
     sl->merges_off = put(merges.data(), merges.size() * sizeof(cart_merge_item));
-    for (int x = 0; x < 2; ++x) {
-        const TileWork &w = st->work_tmp[x];
-        if (sl->tiles[x].n_cta == 0) continue;
-        sl->tiles[x].cta_off = put(w.cta.data(), w.cta.size() * 4);
-        sl->tiles[x].units_off = put(w.units.data(), w.units.size() * sizeof(cart_shared_unit));
-        sl->tiles[x].readers_off = put(w.readers.data(), w.readers.size() * 4);
-        sl->tiles[x].slots_off = put(w.slots.data(), w.slots.size() * 4);
+    if (sl->n_unit_cta > 0) {
+        sl->unit_cta_off = put(w.cta.data(), w.cta.size() * 4);
+        sl->units_off = put(w.units.data(), w.units.size() * sizeof(cart_shared_unit));
+        sl->readers_off = put(w.readers.data(), w.readers.size() * 4);
+        sl->slots_off = put(w.slots.data(), w.slots.size() * 4);
     }
     if (!fits || merges.size() > (size_t)lay.merges_cap)
         return ctx_fail(ctx, CART_ERR_CAPACITY, "q8 attention: the batch's plan exceeds the tables' room");
@@ -742,18 +830,17 @@ cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t laye
     const Q8Layout &lay = st->lay;
     float *part_o = reinterpret_cast<float *>(st->base + lay.part_o_off), *part_lse2 = reinterpret_cast<float *>(st->base + lay.part_lse_off);
     const cart_merge_item *merges = reinterpret_cast<const cart_merge_item *>(sl->dev + sl->merges_off);
-    const bool tiles = sl->tiles[0].n_cta > 0 || sl->tiles[1].n_cta > 0;
+    const bool tiles = sl->n_unit_cta > 0;
     // Partials of the tile kernel, or many: a merge kernel.  Few, all of the stream kernel: whichever block comes last merges.
     const bool merge_after = sl->n_merges > 0 && (tiles || sl->n_merges > cv.n_cta);
     const float scale_log2 = cv.scale * 1.4426950408889634f;
     use_slot(st, sl, s);
-    for (const Slot::Tiles &t : sl->tiles) {
-        if (t.n_cta == 0) continue;
+    if (tiles) {
         Q8TileParams p;
-        p.unit_cta_begin = reinterpret_cast<const uint32_t *>(sl->dev + t.cta_off);
-        p.units = reinterpret_cast<const cart_shared_unit *>(sl->dev + t.units_off);
-        p.readers = reinterpret_cast<const uint32_t *>(sl->dev + t.readers_off);
-        p.reader_slot = reinterpret_cast<const uint32_t *>(sl->dev + t.slots_off);
+        p.unit_cta_begin = reinterpret_cast<const uint32_t *>(sl->dev + sl->unit_cta_off);
+        p.units = reinterpret_cast<const cart_shared_unit *>(sl->dev + sl->units_off);
+        p.readers = reinterpret_cast<const uint32_t *>(sl->dev + sl->readers_off);
+        p.reader_slot = reinterpret_cast<const uint32_t *>(sl->dev + sl->slots_off);
         p.pages = reinterpret_cast<const uint32_t *>(sl->dev);
         p.arena = static_cast<const uint8_t *>(cv.cfg->arena);
         p.q = q;
@@ -767,7 +854,7 @@ cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t laye
         p.n_kv_heads = cv.cfg->n_kv_heads;
         p.n_q_heads = cv.cfg->n_q_heads;
         p.scale_log2 = scale_log2;
-        Q8_CUDA(ctx, q8_launch_tile(p, format, t.n_cta, s));
+        Q8_CUDA(ctx, q8_launch_tile(p, format, sl->n_unit_cta, s));
         ++*cv.launches;
     }
     if (sl->n_cta_used > 0) {

@@ -549,41 +549,46 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
         };
         // A chain's rows into the swizzled K-major operand -- block w (64 dims), 16-byte chunk c at position c ^ (row % 8) -- as
         // fp16 over the power of two that brings a row's largest value to 1 .. 2 (see cart_q8.cu); a row with a NaN or an
-        // infinity as NaN, rows past the readers as zeros.  The warp brings its 32 rows together, 16 lanes a row, all loads in
-        // flight.  Returns what takes the thread's own row's scores to base-2 exponents: 2^e scale log2(e).
-        const uint32_t q_base = base + kOffQ + x * kTileBytes + 32u * sw * 128u;
+        // infinity as NaN, rows past the readers as zeros.  The warp brings its 32 rows together, 16 lanes a row: all copies
+        // in flight, then converted in place.  (Two short loops: this runs once per chain, and straight code that is not in
+        // the instruction cache took 11000 cycles.)  Returns what takes the thread's own row's scores to base-2 exponents:
+        // 2^e scale log2(e).
+        const uint32_t q_mine = base + kOffQ + x * kTileBytes + 32u * sw * 128u + ((uint32_t)lane & 8u) * (kBlock / 8u);   // dims < 64 or not
         auto bring_q = [&](uint32_t kv_head, uint32_t batch, bool on) -> float {
             const uint32_t c = (uint32_t)lane & 15u, up = (uint32_t)lane >> 4;
             const uint32_t from = on ? batch * (uint32_t)p.n_q_heads + kv_head * G + h : ~0u;   // the row's place among all of q's
-            int my_exp = 0;
-            uint4 v[16];
-#pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) {
-                const uint32_t src = __shfl_sync(0xffffffffu, from, (int)(2u * i + up));
-                v[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (src != ~0u) v[i] = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) + (size_t)src * kHeadDim) + c);
+            auto at = [&](uint32_t r) { return q_mine + r * 128u + (((c & 7u) ^ (r & 7u)) << 4); };
+#pragma unroll 2
+            for (uint32_t r = up; r < 32u; r += 2u) {
+                const uint32_t src = __shfl_sync(0xffffffffu, from, (int)r);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at(r)),
+                             "l"(reinterpret_cast<const __nv_bfloat16 *>(p.q) + (size_t)(src == ~0u ? 0u : src) * kHeadDim + 8u * c),
+                             "r"(src == ~0u ? 0u : 16u)
+                             : "memory");
             }
-#pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) {
-                uint32_t big = __vmaxu2(__vmaxu2(v[i].x & 0x7FFF7FFFu, v[i].y & 0x7FFF7FFFu), __vmaxu2(v[i].z & 0x7FFF7FFFu, v[i].w & 0x7FFF7FFFu));
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();
+            int my_exp = 0;
+#pragma unroll 2
+            for (uint32_t r = up; r < 32u; r += 2u) {
+                uint32_t w[4];
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at(r)) : "memory");
+                uint32_t big = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
                 big = max(big & 0xFFFFu, big >> 16);
-                big = __reduce_max_sync(0xFFFFu << (16u * up), big);
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
                 const int qe = big >= 0x7F80u ? 0 : min(max((int)(big >> 7), 2) - 127, 126);
                 const float down = big >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - qe) << 23);
-                const uint32_t r = 2u * i + up;
                 const int other = __shfl_xor_sync(0xffffffffu, qe, 16);
                 if ((uint32_t)lane == r) my_exp = qe;
                 if ((uint32_t)lane == (r ^ 1u)) my_exp = other;   // (the other half warp's row of the pair)
-                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
                 uint32_t o[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const __half2 y = __floats2half2_rn(__uint_as_float(w[j] << 16) * down, __uint_as_float(w[j] & 0xFFFF0000u) * down);
                     o[j] = *reinterpret_cast<const uint32_t *>(&y);
                 }
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_base + (c >> 3) * kBlock + r * 128u + (((c & 7u) ^ (r & 7u)) << 4)),
-                             "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
-                             : "memory");
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at(r)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
             }
             fence_async_smem();
             __syncwarp();

@@ -316,6 +316,36 @@ def binding_without_sharing(p, ids, q):
     return got
 
 
+@pytest.mark.parametrize("fmt,hq,hkv,users,n", [("int8", 8, 4, 100, (1500, 333, 64)), ("e4m3", 12, 4, 90, (1700, 129, 40)),
+                                                 ("int8", 8, 8, 40, (2000, 700)), ("e4m3", 2, 2, 260, (1200, 128))])
+def test_parts_shared_by_enough_rows_for_the_tensor_cores(pair, fmt, hq, hkv, users, n):
+    # shared parts on the tcgen05 kernel, the rest streamed, all merged: rows without tokens of their own, rows that name a part
+    # twice, rows behind one shared part alone among rows that have more, a message in between
+    p = pair(hq, hkv, fmt, rows=users + 40, mb=160)
+    z = [p.open() for _ in n]
+    p.write(z, [rand((m, hkv, 128), m, 4) for m in n], [rand((m, hkv, 128), m + 9, 4) for m in n])
+    parts = [z if i % 3 == 0 else [z[0]] if i % 3 == 1 else [z[0], z[-1], z[0]] for i in range(users)]
+    ids = [p.open(x) for x in parts]
+    own = [(13 * i) % 90 if i % 4 else 0 for i in range(users)]
+    p.write(ids, [rand((m, hkv, 128), 60 + m) for m in own], [rand((m, hkv, 128), 70 + m) for m in own])
+    new = [1] * users
+    new[5], new[9] = 30, 3
+    own[5], own[9] = max(own[5], 30), max(own[9], 3)
+    p.write([ids[5], ids[9]], [rand((own[i], hkv, 128), 80) for i in (5, 9)], [rand((own[i], hkv, 128), 81) for i in (5, 9)], [0, 0])
+    q = rand((sum(new), hq, 128), 8)
+    out, lse = p.attend(ids, q, new, extra=3)
+    before = B.cart_launch_count(p.ctx)
+    again, _ = p.attend(ids, q, new)
+    assert torch.equal(out, again) and B.cart_launch_count(p.ctx) - before == 3   # tiles, stream, merge
+    some = [0, 1, 2, 4, 5, 6, 7, 9, 10, users - 1]
+    at = np.concatenate([[0], np.cumsum(new)])
+    rows = np.concatenate([np.arange(at[i], at[i + 1]) for i in some])
+    p.check([ids[i] for i in some], q[rows], out[rows], lse[rows], [new[i] for i in some])
+    B.cart_set_share_min_readers(p.ctx, 0)
+    apart, _ = p.attend(ids, q, new)
+    assert float((apart.float() - out.float()).norm() / out.float().norm()) < 0.01
+
+
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 @pytest.mark.parametrize("hq,hkv", [(3, 1), (5, 1), (16, 2), (4, 4)])
 @pytest.mark.parametrize("n,new,parts", [(4, 4, []), (700, 4, [1]), (130, 130, [128]), (600, 257, [300, 5]), (1500, 60, [64, 1, 900])])
