@@ -549,51 +549,60 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
         };
         // A chain's rows into the swizzled K-major operand -- block w (64 dims), 16-byte chunk c at position c ^ (row % 8) -- as
         // fp16 over the power of two that brings a row's largest value to 1 .. 2 (see cart_q8.cu); a row with a NaN or an
-        // infinity as NaN, rows past the readers as zeros.  The warp brings its 32 rows together, 16 lanes a row: all copies
-        // in flight, then converted in place.  (Two short loops: this runs once per chain, and straight code that is not in
-        // the instruction cache took 11000 cycles.)  Returns what takes the thread's own row's scores to base-2 exponents:
-        // 2^e scale log2(e).
-        const uint32_t q_mine = base + kOffQ + x * kTileBytes + 32u * sw * 128u + ((uint32_t)lane & 8u) * (kBlock / 8u);   // dims < 64 or not
+        // infinity as NaN, rows past the readers as zeros.  The warp copies its 32 rows together, 16 lanes a row, all copies in
+        // flight; then every thread converts its own row in place.  (Short loops: this runs once per chain, and straight code
+        // that is not in the instruction cache took 11000 cycles; a reduction across the 16 lanes of a row 9000.)  Returns what
+        // takes the row's scores to base-2 exponents: 2^e scale log2(e).
+        const uint32_t q_warp = base + kOffQ + x * kTileBytes + 32u * sw * 128u;
         auto bring_q = [&](uint32_t kv_head, uint32_t batch, bool on) -> float {
-            const uint32_t c = (uint32_t)lane & 15u, up = (uint32_t)lane >> 4;
+            const uint32_t c = (uint32_t)lane & 15u;
             const uint32_t from = on ? batch * (uint32_t)p.n_q_heads + kv_head * G + h : ~0u;   // the row's place among all of q's
-            auto at = [&](uint32_t r) { return q_mine + r * 128u + (((c & 7u) ^ (r & 7u)) << 4); };
-#pragma unroll 2
-            for (uint32_t r = up; r < 32u; r += 2u) {
+            auto at = [&](uint32_t r, uint32_t chunk) { return q_warp + (chunk >> 3) * kBlock + r * 128u + (((chunk & 7u) ^ (r & 7u)) << 4); };
+#pragma unroll 4
+            for (uint32_t r = (uint32_t)lane >> 4; r < 32u; r += 2u) {
                 const uint32_t src = __shfl_sync(0xffffffffu, from, (int)r);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at(r)),
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at(r, c)),
                              "l"(reinterpret_cast<const __nv_bfloat16 *>(p.q) + (size_t)(src == ~0u ? 0u : src) * kHeadDim + 8u * c),
                              "r"(src == ~0u ? 0u : 16u)
                              : "memory");
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();
-            int my_exp = 0;
-#pragma unroll 2
-            for (uint32_t r = up; r < 32u; r += 2u) {
-                uint32_t w[4];
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at(r)) : "memory");
-                uint32_t big = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
-                big = max(big & 0xFFFFu, big >> 16);
+            // four chunks at a time, their loads together
+            uint32_t big = 0u, w[4][4];
+            auto get = [&](uint32_t k0) {
 #pragma unroll
-                for (int d = 1; d < 16; d <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
-                const int qe = big >= 0x7F80u ? 0 : min(max((int)(big >> 7), 2) - 127, 126);
-                const float down = big >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - qe) << 23);
-                const int other = __shfl_xor_sync(0xffffffffu, qe, 16);
-                if ((uint32_t)lane == r) my_exp = qe;
-                if ((uint32_t)lane == (r ^ 1u)) my_exp = other;   // (the other half warp's row of the pair)
-                uint32_t o[4];
+                for (uint32_t k = 0; k < 4; ++k)
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3]) : "r"(at((uint32_t)lane, k0 + k)));
+            };
+#pragma unroll 1
+            for (uint32_t k0 = 0; k0 < 16u; k0 += 4u) {
+                get(k0);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const __half2 y = __floats2half2_rn(__uint_as_float(w[j] << 16) * down, __uint_as_float(w[j] & 0xFFFF0000u) * down);
-                    o[j] = *reinterpret_cast<const uint32_t *>(&y);
-                }
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at(r)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                for (int k = 0; k < 4; ++k)
+                    big = __vmaxu2(big, __vmaxu2(__vmaxu2(w[k][0] & 0x7FFF7FFFu, w[k][1] & 0x7FFF7FFFu), __vmaxu2(w[k][2] & 0x7FFF7FFFu, w[k][3] & 0x7FFF7FFFu)));
+            }
+            big = max(big & 0xFFFFu, big >> 16);
+            const int qe = big >= 0x7F80u ? 0 : min(max((int)(big >> 7), 2) - 127, 126);
+            const float down = big >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - qe) << 23);
+#pragma unroll 1
+            for (uint32_t k0 = 0; k0 < 16u; k0 += 4u) {
+                get(k0);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const __half2 y = __floats2half2_rn(__uint_as_float(w[k][j] << 16) * down, __uint_as_float(w[k][j] & 0xFFFF0000u) * down);
+                        w[k][j] = *reinterpret_cast<const uint32_t *>(&y);
+                    }
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k)
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at((uint32_t)lane, k0 + k)), "r"(w[k][0]), "r"(w[k][1]), "r"(w[k][2]), "r"(w[k][3]));
             }
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kBarQReady + (int)x));
-            return __uint_as_float((uint32_t)(my_exp + 127) << 23) * p.scale_log2;
+            return __uint_as_float((uint32_t)(qe + 127) << 23) * p.scale_log2;
         };
         auto has_rows = [&](const cart_shared_unit &u) { return x == 0u || u.n_readers > tpt; };   // the M-tile takes part
         uint32_t halves = 0;     // halves of tiles of this M-tile so far
