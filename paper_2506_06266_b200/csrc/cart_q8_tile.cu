@@ -12,10 +12,12 @@
 //                      scales, 8-byte stores into the swizzled tiles.  The next loads are in flight meanwhile.
 //                      No raw tile is staged in shared memory: its bandwidth is what the products need (per tile and
 //                      pair of M-tiles 192 KB of operands are read and 64 KB written, as long as the products take).
-//   2 MMA threads      one per M-tile, of different warps (issuing the two M-tiles' 48 instructions a tile from one thread
-//                      took 1.5 times as long as executing them).  A tile's keys are dealt with in halves: S of 64 keys, its softmax, P V of these 64 tokens.  As soon as
-//                      a half's P is there, its P V is issued and behind it S of the same half of the next tile, into the
-//                      same columns; the softmax meanwhile has the other half.  So neither waits for the other's latency
+//   4 MMA threads      for each M-tile one that issues S and one that issues P V, of different warps: issuing an
+//                      instruction takes a thread 50 to 100 cycles beside the other warps, its execution 48 or 64 (one thread
+//                      for all of them: 213 us for six ragged messages, two: 167).  A tile's keys are dealt with in halves: S
+//                      of 64 keys, its softmax, P V of these 64 tokens.  As soon as
+//                      a half's P is there, its P V is issued, and when that is done S of the same half of the next tile, into
+//                      the same columns; the softmax meanwhile has the other half.  So neither waits for the other's latency
 //                      (with whole tiles a row's softmax, P V and S took turns: 6000 cycles a tile, 2048 of them
 //                      exponentials).  V is a K-major operand [dim][token], because a word of the stored values holds four
 //                      tokens of one dim; inside a block of 16 the tokens stand in the stored order 0 1 8 9  2 3 10 11
@@ -52,7 +54,7 @@ constexpr uint32_t kTileBytes = 2u * kBlock;          // 128 x 128 bf16
 constexpr int kKStages = 3;
 constexpr int kVStages = 2;
 constexpr int kConvWarps = 8;
-constexpr int kThreads = 640;                         // utility warpgroup (warps 0, 1: MMA), 2 softmax and 2 converter warpgroups
+constexpr int kThreads = 640;                         // utility warpgroup (MMA), 2 softmax and 2 converter warpgroups
 // Registers per thread after the warpgroups have re-divided the launch's 640 x 96 = 61440:
 // 128 x 56 + 256 x 136 + 256 x 72 = 60416.
 constexpr int kRegsUtility = 56;
@@ -84,9 +86,9 @@ enum Bar : int {
                      // scores are there, and so is P V of the same half of the tile before
     kBarPReady = 14, // [M-tile][half] softmax -> MMA (4 arrivals: one per warp)
     kBarQReady = 18, // [M-tile] softmax -> MMA: a chain's query rows are in place (4 arrivals)
-    kBarOFull = 20,  // [M-tile][half] MMA (commit of P V) -> softmax.  (A barrier per half: whoever waits for one has seen
+    kBarOFull = 20,  // [M-tile][half] MMA (commit of P V) -> softmax and S.  (A barrier per half: whoever waits for one has seen
                      // scores that were issued behind the phase before, so its parity is not ambiguous.)
-    kBarDrain = 24,  // [M-tile] MMA (commit) -> MMA, on the way out
+    kBarDrain = 24,  // [warp] MMA (commit) -> MMA, on the way out
 };
 
 // Instruction descriptors: fp32 accumulator, both operands K-major, M = 128; fp16, N = 64 (S), or bf16, N = 128 (P V).
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
             mbar_init(bar(kBarOFull + i), 1);
         }
         for (int i = 0; i < 2; ++i) mbar_init(bar(kBarQReady + i), 4);
-        for (int i = 0; i < 2; ++i) mbar_init(bar(kBarDrain + i), 1);
+        for (int i = 0; i < 4; ++i) mbar_init(bar(kBarDrain + i), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -296,100 +298,72 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUtility));
-        if (warp < 2 && lane == 0) {
-            // ================= MMA issuers: warp x's first thread for M-tile x ================================
-            const uint32_t x = (uint32_t)warp;
+        if (lane == 0) {
+            // ================= MMA issuers: for M-tile x, warp x issues its P V products, warp 2 + x its S ====
+            const uint32_t x = (uint32_t)warp & 1u;
+            const bool scores = warp >= 2;
             bool ok = true;
             auto wait = [&](int b, uint32_t parity) -> bool {
                 return mbar_wait(bar(b), parity, abort_flag, p.status, kStatusTimeoutMma);
             };
-            // where the next scores are: unit, tile in it, tiles of the unit; whether the M-tile takes part in it, whether it
-            // begins a chain
-            uint32_t ui = unit_begin, t = 0, n = 0;
-            bool mine = false, fresh = true;
-            auto unit = [&]() {
-                if (ui >= unit_end) return;
-                const cart_shared_unit u = p.units[ui];
-                n = u.n_tiles;
-                mine = x == 0u || u.n_readers > tpt;
-                fresh = !(u.flags & CART_UNIT_CONT);
-            };
-            unit();
-            uint32_t q_par = 0, p_par = 0;   // parities: of the chains whose rows, of the tiles whose P, have been delivered
-            uint32_t kst = 0, kpar = 0, vst = 0, vpar = 0;
+            const int full = scores ? kBarKFull : kBarVFull, empty = scores ? kBarKEmpty : kBarVEmpty;
+            const uint32_t stages = scores ? (uint32_t)kKStages : (uint32_t)kVStages;
+            const uint32_t ring = base + (scores ? kOffK : kOffV), half = scores ? kBlock / 2u : kBlock;   // the second 64 tokens
             const uint64_t q_desc = umma_desc(base + kOffQ + x * kTileBytes, 16, 1024);
-            // S of half y of the tile in front: its columns last held P, which a P V product issued earlier reads
-            auto issue_s = [&](uint32_t y) {
-                tc_fence_after();
-                product_s(tmem + x * 128u + y * 64u, q_desc, umma_desc(base + kOffK + kst * kTileBytes + y * (kBlock / 2u), 16, 1024));
-                mma_commit(bar(kBarSFull + (int)(2u * x + y)));
-                mbar_arrive(bar(kBarSFull + (int)(2u * x + y)));
-            };
-            // (Written once, for both halves and for the first tile too: the roles share an instruction cache.)
-            bool have = false, cur_mine = false, cur_first = false;   // the current tile: there is one, ...
-            while (ok && (have || ui < unit_end)) {
-                const bool more = ui < unit_end, nxt_mine = mine, nxt_first = t == 0u && fresh;
-                bool k_here = false;
-                if (have) {
-                    // the current tile's P V and, in the same chain, the next tile's S
-                    ok = wait(kBarVFull + (int)vst, vpar);
+            uint32_t st = 0, par = 0;        // the ring's next stage
+            uint32_t q_par = 0, t_par = 0;   // parities: of the M-tile's chains, of its tiles
+            bool begun = false;              // a tile of the M-tile has been issued
+            for (uint32_t ui = unit_begin; ui < unit_end && ok; ++ui) {
+                const cart_shared_unit u = p.units[ui];
+                const bool mine = x == 0u || u.n_readers > tpt;
+                bool first = !(u.flags & CART_UNIT_CONT);   // the next tile begins a chain
 #pragma unroll 1
-                    for (uint32_t y = 0; y < 2 && ok && cur_mine; ++y) {
-                        ok = wait(kBarPReady + (int)(2u * x + y), p_par);
-                        if (!ok) break;
-                        tc_fence_after();
-                        product_pv(tmem + kTmemO + 128u * x, tmem + x * 128u + y * 64u,
-                                   umma_desc(base + kOffV + vst * kTileBytes + y * kBlock, 16, 1024), (cur_first && y == 0u) ? 0u : 1u);
-                        mma_commit(bar(kBarOFull + (int)(2u * x + y)));
-                        if (more && !nxt_first) {
-                            if (!k_here) ok = wait(kBarKFull + (int)kst, kpar);
+                for (uint32_t t = 0; t < u.n_tiles && ok; ++t) {
+                    ok = wait(full + (int)st, par);
+                    if (ok && mine && scores && first) {   // a new chain: its rows first
+                        ok = wait(kBarQReady + (int)x, q_par);
+                        q_par ^= 1u;
+                    }
+#pragma unroll 1
+                    for (uint32_t y = 0; y < 2 && ok && mine; ++y) {
+                        const uint64_t desc = umma_desc(ring + st * kTileBytes + y * half, 16, 1024);
+                        const uint32_t cols = tmem + x * 128u + y * 64u;
+                        if (scores) {
+                            // (these columns last held P, until its P V was done)
+                            if (begun) ok = wait(kBarOFull + (int)(2u * x + y), t_par ^ 1u);
                             if (!ok) break;
-                            k_here = true;
-                            issue_s(y);
+                            tc_fence_after();
+                            product_s(cols, q_desc, desc);
+                            mma_commit(bar(kBarSFull + (int)(2u * x + y)));
+                            mbar_arrive(bar(kBarSFull + (int)(2u * x + y)));
+                        } else {
+                            ok = wait(kBarPReady + (int)(2u * x + y), t_par);
+                            if (!ok) break;
+                            tc_fence_after();
+                            product_pv(tmem + kTmemO + 128u * x, cols, desc, (first && y == 0u) ? 0u : 1u);
+                            mma_commit(bar(kBarOFull + (int)(2u * x + y)));
                         }
                     }
                     if (!ok) break;
                     // (a stage is free when both M-tiles are done with it; one that takes no part says so at once)
-                    if (cur_mine) {
-                        mma_commit(bar(kBarVEmpty + (int)vst));
-                        p_par ^= 1u;
+                    if (mine) {
+                        mma_commit(bar(empty + (int)st));
+                        t_par ^= 1u;
+                        begun = true;
+                        first = false;
                     } else {
-                        mbar_arrive(bar(kBarVEmpty + (int)vst));
+                        mbar_arrive(bar(empty + (int)st));
                     }
-                    if (++vst == (uint32_t)kVStages) {
-                        vst = 0;
-                        vpar ^= 1u;
+                    if (++st == stages) {
+                        st = 0;
+                        par ^= 1u;
                     }
                 }
-                have = more;
-                if (!more) break;
-                if (!k_here) ok = wait(kBarKFull + (int)kst, kpar);
-                if (ok && nxt_first && nxt_mine) {   // a new chain: its rows first
-                    ok = wait(kBarQReady + (int)x, q_par);
-                    q_par ^= 1u;
-                    if (!ok) break;
-                    issue_s(0u);
-                    issue_s(1u);
-                }
-                if (!ok) break;
-                if (nxt_mine) mma_commit(bar(kBarKEmpty + (int)kst));
-                else mbar_arrive(bar(kBarKEmpty + (int)kst));
-                if (++kst == (uint32_t)kKStages) {
-                    kst = 0;
-                    kpar ^= 1u;
-                }
-                if (++t == n) {
-                    ++ui;
-                    t = 0;
-                    unit();
-                }
-                cur_mine = nxt_mine;
-                cur_first = nxt_first;
             }
             // products still in flight must finish before the tensor memory is given back
-            mma_commit(bar(kBarDrain + (int)x));
+            mma_commit(bar(kBarDrain + warp));
             const uint64_t t0 = global_timer_ns();
-            while (!mbar_try_wait(bar(kBarDrain + (int)x), 0) && global_timer_ns() - t0 < kWaitLimitNs) {}
+            while (!mbar_try_wait(bar(kBarDrain + warp), 0) && global_timer_ns() - t0 < kWaitLimitNs) {}
         }
     } else if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
