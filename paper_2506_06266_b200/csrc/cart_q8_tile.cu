@@ -23,8 +23,9 @@
 //                      tokens of one dim; inside a block of 16 the tokens stand in the stored order 0 1 8 9  2 3 10 11
 //                      4 5 12 13  6 7 14 15, and the softmax threads pack their probabilities in that order, which costs
 //                      nothing.
-//   2 x 4 softmax      one warpgroup per M-tile, one thread per row.  A row's reference m moves only when outgrown by more
-//   warps              than 2^8; its thread then rescales the accumulator.
+//   2 x 4 softmax      one warpgroup per M-tile, one thread per row.  A row's reference m is a whole number that moves only when
+//   warps              a sum shows that it has been outgrown by far; its thread then rescales the accumulator.  (bf16 and fp32
+//                      hold what may grow up to then; looking for every tile's maximum first took 480 of a half's 2550 cycles.)
 //
 // The scales join the softmax, where a block's 16 tokens are 16 columns of a thread's row: keys' scales multiply the
 // scores (in place of the softmax's own factor), values' scales are added in the exponent, so that P is held times the
@@ -62,7 +63,7 @@ constexpr int kRegsSoftmax = 136;
 constexpr int kRegsConvert = 72;
 constexpr uint32_t kTmemCols = 512;                   // S_A S_B (scores, then P), O_A O_B: 128 fp32 columns each
 constexpr uint32_t kTmemO = 2u * 128u;
-constexpr float kRescaleStep = 8.f;
+constexpr float kLargeSum = 1048576.f;                // a sum of 16 probabilities beyond this raises the row's reference
 
 // shared-memory layout (offsets from a 1024-byte aligned base)
 constexpr uint32_t kOffQ = 0;                          // query rows of the two M-tiles
@@ -581,8 +582,8 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
         auto has_rows = [&](const cart_shared_unit &u) { return x == 0u || u.n_readers > tpt; };   // the M-tile takes part
         uint32_t halves = 0;     // halves of tiles of this M-tile so far
         uint32_t tiles = 0;      // tiles of the block so far
-        float m_run = -INFINITY, l_run = 0.f;
-        bool fresh = true;       // no tile of the chain has been seen yet
+        float m_run = -INFINITY, l_run = 0.f;   // the row's reference (a whole number; -inf: it has seen no key yet) and sum
+        uint32_t s[2][32];
         bool marked = false;     // the row has seen values without a scale
         float f_row = 0.f, f_next = 0.f;   // see bring_q: of this chain's rows, of the next one's
         uint32_t uq_next = unit_begin;   // the unit whose rows are fetched next (a chain's first that this M-tile takes part in)
@@ -615,7 +616,6 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 m_run = -INFINITY;
                 l_run = 0.f;
                 f_row = f_next;
-                fresh = true;
                 marked = false;
                 // the next chain's rows: what the copy hangs on is read now, long before its last tile
                 uq_next = first_chain(ui + u.reserved);
@@ -638,6 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 const bool in = i_reader < (u.tr_hi & 0xFFFFu) && i_reader >= u.tr_hi >> 16;
                 limit = in && lb >= 0 ? (lb < u.lim_cap ? lb : u.lim_cap) : -1;
             }
+            // (32 keys at a time: the second 32 are on their way from tensor memory while the first are dealt with)
             for (uint32_t t = 0; t < u.n_tiles; ++t, ++tiles) {
 #pragma unroll 1
                 for (uint32_t y = 0; y < 2; ++y, ++halves) {
@@ -645,98 +646,108 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                     if (!alive) continue;
                     tc_fence_after();
                     const uint32_t cols = s_addr + 64u * y;
-                    uint32_t s[2][32];
                     tmem_ld32_issue(cols, s[0]);
-                    tmem_ld32_issue(cols + 32u, s[1]);
-                    const int32_t seen = limit - (int32_t)(t * (uint32_t)kTile + 64u * y);   // the last of the 64 keys that this row sees
                     const uint32_t meta = base + kOffMeta + (tiles & 7u) * 128u + 64u * y;
-                    float4 mt[4];
+                    const int32_t seen_half = limit - (int32_t)(t * (uint32_t)kTile + 64u * y);   // the last of the half's keys that this row sees
 #pragma unroll
-                    for (uint32_t b = 0; b < 4; ++b)
-                        asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(mt[b].x), "=f"(mt[b].y), "=f"(mt[b].z), "=f"(mt[b].w) : "r"(meta + 16u * b));
-                    tmem_ld_wait(s[0]);
-                    tmem_ld_wait(s[1]);
-                    // Scores of keys that the row does not see (whatever stands there): -inf.  Few tiles have any; the warp
-                    // decides together, so that the others pay one vote.
-                    if (__any_sync(0xffffffffu, seen < 63)) {
+                    for (int z = 0; z < 2; ++z) {
+                        uint32_t(&v)[32] = s[z];
+                        const int32_t seen = seen_half - 32 * z;
+                        float4 mt[2];
 #pragma unroll
-                        for (int k = 0; k < 64; ++k)
-                            if (k > seen) s[k >> 5][k & 31] = 0xFF800000u;
-                        // (a block of which the row sees nothing may have no scale, or none at all: -inf has to stay -inf)
+                        for (uint32_t b = 0; b < 2; ++b)
+                            asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(mt[b].x), "=f"(mt[b].y), "=f"(mt[b].z), "=f"(mt[b].w) : "r"(meta + 32u * z + 16u * b));
+                        tmem_ld_wait(v);
+                        if (z == 0) tmem_ld32_issue(cols + 32u, s[1]);
+                        // Scores of keys that the row does not see (whatever stands there): -inf.  Few tiles have any; the warp
+                        // decides together, so that the others pay one vote.
+                        if (__any_sync(0xffffffffu, seen < 31)) {
 #pragma unroll
-                        for (int b = 0; b < 4; ++b)
-                            if (16 * b > seen) {
-                                mt[b].x = 1.f;
-                                mt[b].w = 0.f;
-                            }
-                    }
-                    float mx = -INFINITY;
+                            for (int k = 0; k < 32; ++k)
+                                if (k > seen) v[k] = 0xFF800000u;
+                            // (a block of which the row sees nothing may have no scale, or none at all: -inf has to stay -inf)
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const uint32_t *r = s[b >> 1] + 16 * (b & 1);
-                        float a = max3(__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[2]));
-                        float e = max3(__uint_as_float(r[3]), __uint_as_float(r[4]), __uint_as_float(r[5]));
-                        a = max3(a, __uint_as_float(r[6]), __uint_as_float(r[7]));
-                        e = max3(e, __uint_as_float(r[8]), __uint_as_float(r[9]));
-                        a = max3(a, __uint_as_float(r[10]), __uint_as_float(r[11]));
-                        e = max3(e, __uint_as_float(r[12]), __uint_as_float(r[13]));
-                        a = max3(a, __uint_as_float(r[14]), __uint_as_float(r[15]));
-                        // (a key block without a scale: a NaN, which takes no part in the maximum and stays in the sums)
-                        mt[b].x *= f_row;
-                        mx = fmaxf(mx, fmaxf(a, e) * mt[b].x);
-                        if (mt[b].w != 0.f) marked = true;
-                    }
-                    if (fresh) {
-                        m_run = mx;
-                        fresh = false;
-                    } else if (__any_sync(0xffffffffu, mx > m_run + kRescaleStep)) {
-                        // a row of this warp has outgrown its reference: all of them move up and rescale, once P V of the half
-                        // before is complete (P V of the one before that is: these scores were issued behind it)
-                        const float m_new = fmaxf(m_run, mx);
-                        const float f = m_new == -INFINITY ? 1.f : fast_exp2(m_run - m_new);
-                        m_run = m_new;
-                        l_run *= f;
-                        alive = warp_wait(kBarOFull + (int)(2u * x + (y ^ 1u)), ((halves - 1u) >> 1) & 1u);
-                        if (!alive) continue;
-                        tc_fence_after();
-#pragma unroll 1
-                        for (uint32_t c = 0; c < 8; ++c) {
-                            uint32_t o[16];
-                            tmem_ld16(o_addr + c * 16u, o);
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            tmem_st16(o_addr + c * 16u, o);
+                            for (int b = 0; b < 2; ++b)
+                                if (16 * b > seen) {
+                                    mt[b].x = 1.f;
+                                    mt[b].w = 0.f;
+                                }
                         }
-                    }
-                    // probabilities times their values' scales as bf16 pairs, in the stored order of the tokens: pair 2 i of a
-                    // block of 16 holds tokens 2 i and 2 i + 1, pair 2 i + 1 tokens 2 i + 8 and 2 i + 9
-                    const float m_use = m_run == -INFINITY ? 0.f : m_run;
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
+                        if (mt[0].w + mt[1].w != 0.f) marked = true;
+                        const float c0 = f_row * mt[0].x, c1 = f_row * mt[1].x;
                         uint32_t w[16];
+                        float sum0, sum1;
+                        // Probabilities times their values' scales as bf16 pairs, in the stored order of the tokens: pair 2 i of a
+                        // block of 16 holds tokens 2 i and 2 i + 1, pair 2 i + 1 tokens 2 i + 8 and 2 i + 9.  They are taken against
+                        // the reference as it is, without looking for the maximum first: only where a sum turns out large, or
+                        // the row has no reference yet, the reference is raised and the 32 are done again.
+                        const bool unset = m_run == -INFINITY && seen >= 0;
+#pragma unroll 1
+                        for (int pass = 0;; ++pass) {
+                            const float m_use = m_run == -INFINITY ? 0.f : m_run;
 #pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const float cc = mt[2 * c + z].x, dd = mt[2 * c + z].y - m_use;
-                            const uint64_t cc2 = pair(cc, cc), dd2 = pair(dd, dd);
-                            uint64_t sum = pair(0.f, 0.f);
+                            for (int b = 0; b < 2; ++b) {
+                                const float cc = b ? c1 : c0, dd = mt[b].y - m_use;
+                                const uint64_t cc2 = pair(cc, cc), dd2 = pair(dd, dd);
+                                uint64_t sum_a = pair(0.f, 0.f), sum_b = pair(0.f, 0.f);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const int tok = 16 * z + 2 * (j >> 1) + 8 * (j & 1);
-                                float2 e = unpair(fma2(pair(__uint_as_float(s[c][tok]), __uint_as_float(s[c][tok + 1])), cc2, dd2));
-                                e.x = fast_exp2(e.x);
-                                e.y = fast_exp2(e.y);
-                                sum = add2(sum, pair(e.x, e.y));
-                                w[8 * z + j] = pack_bf16(e.x, e.y);
+                                for (int j = 0; j < 8; ++j) {
+                                    const int tok = 16 * b + 2 * (j >> 1) + 8 * (j & 1);
+                                    float2 e = unpair(fma2(pair(__uint_as_float(v[tok]), __uint_as_float(v[tok + 1])), cc2, dd2));
+                                    e.x = fast_exp2(e.x);
+                                    e.y = fast_exp2(e.y);
+                                    if (j & 1) sum_b = add2(sum_b, pair(e.x, e.y));
+                                    else sum_a = add2(sum_a, pair(e.x, e.y));
+                                    w[8 * b + j] = pack_bf16(e.x, e.y);
+                                }
+                                const float2 t2 = unpair(add2(sum_a, sum_b));
+                                (b ? sum1 : sum0) = (t2.x + t2.y) * mt[b].z;
                             }
-                            const float2 t2 = unpair(sum);
-                            l_run = fmaf(t2.x + t2.y, mt[2 * c + z].z, l_run);
+                            const bool redo = pass == 0 && (unset || sum0 > kLargeSum || sum1 > kLargeSum);
+                            if (!__any_sync(0xffffffffu, redo)) break;
+                            if (pass == 1) break;
+                            // The reference goes up to the maximum, rounded up to a whole number: everything that refers to the old one
+                            // is rescaled by a power of two, exactly.
+                            float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+                            for (int k = 0; k < 16; k += 2) {
+                                mx0 = max3(mx0, __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+                                mx1 = max3(mx1, __uint_as_float(v[16 + k]), __uint_as_float(v[16 + k + 1]));
+                            }
+                            // (a key block without a scale: a NaN, which takes no part in the maximum and stays in the sums)
+                            const float m_new = fmaxf(m_run, ceilf(fmaxf(mx0 * c0, mx1 * c1)));
+                            const float f = m_new == -INFINITY ? 1.f : fast_exp2(m_run - m_new);
+                            m_run = m_new;
+                            l_run *= f;
+                            if (z == 1) {   // the half's first 32 are in place already, in bf16
+                                tmem_st_wait();
+                                const __nv_bfloat162 f2 = __float2bfloat162_rn(f);
+                                uint32_t o[16];
+                                tmem_ld16(cols, o);
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) o[k] = bf162_mul(o[k], *reinterpret_cast<const uint32_t *>(&f2));
+                                tmem_st16(cols, o);
+                            }
+                            // (P V of the half before may not be done yet; whatever was before that is)
+                            if (halves > 0u) alive = alive && warp_wait(kBarOFull + (int)(2u * x + (y ^ 1u)), ((halves - 1u) >> 1) & 1u);
+                            if (!alive) break;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (uint32_t c = 0; c < 8; ++c) {
+                                uint32_t o[16];
+                                tmem_ld16(o_addr + c * 16u, o);
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                                tmem_st16(o_addr + c * 16u, o);
+                            }
                         }
-                        tmem_st16(cols + 16u * (uint32_t)c, w);
+                        l_run += sum0 + sum1;
+                        tmem_st16(cols + 16u * (uint32_t)z, w);
                     }
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(kBarPReady + (int)(2u * x + y)));
+                    if (lane == 0 && alive) mbar_arrive(bar(kBarPReady + (int)(2u * x + y)));
                 }
             }
             // the chain's query rows have been read for the last time (its last scores have been here): the next one's come
