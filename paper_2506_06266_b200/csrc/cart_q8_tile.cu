@@ -370,8 +370,11 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
         // ================= converters: codes -> bf16 operand tiles ======================================
         // Warp w takes block w of every tile, its keys and then its values.
+        // A lane takes the bytes of the stored order that belong to (g, t4) = (lane / 4, lane % 4) there, but with even g in the
+        // lower half warp and odd g in the upper: the 8-byte stores of a half warp then fall on all banks of the swizzled
+        // tiles (in the stored order on half of them).
         const uint32_t b = (uint32_t)warp - 12u;
-        const uint32_t g = (uint32_t)lane >> 2, t4 = (uint32_t)lane & 3u;
+        const uint32_t g = ((uint32_t)lane >> 1 & 6u) | (uint32_t)lane >> 4, t4 = (uint32_t)lane & 3u, place = 4u * g + t4;
         pdl_wait();  // the codes may come from the kernel before
         // where the tile whose codes are requested next lies
         uint32_t ui = unit_begin, t = 0, n = 0, row = 0, tok_end = 0, page = 0, page_next = 0;
@@ -390,9 +393,6 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
             page_next = page_of(1u);
         };
         unit();
-        // Lanes of odd g hold the chunks 1 0 3 2 of the keys instead of 0 1 2 3: the 8-byte stores of a half warp then fall
-        // on all banks (with all lanes at the same dims, on half of them).
-        const uint32_t odd = g & 1u;
         uint4 ck[4], cv[4];
         uint32_t scales = 0, left = 0;   // of the tile whose keys were requested last: scale bytes; tokens of the block (may exceed 16)
         const uint8_t *blk = nullptr;
@@ -404,9 +404,9 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
             scales = 0u;
             if (left > 0u) {
                 blk = head + (size_t)page * kRowBytes;
-                const uint4 *src = reinterpret_cast<const uint4 *>(blk) + lane;
+                const uint4 *src = reinterpret_cast<const uint4 *>(blk) + place;
 #pragma unroll
-                for (uint32_t c = 0; c < 4; ++c) ck[c] = __ldcg(src + 32u * (c ^ odd));
+                for (uint32_t c = 0; c < 4; ++c) ck[c] = __ldcg(src + 32u * c);
                 scales = __ldcg(reinterpret_cast<const unsigned short *>(blk + kQ8ScaleOff));
             }
             page = page_next;
@@ -424,19 +424,19 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
         auto wait_conv = [&](int x, uint32_t parity) -> bool {
             return __all_sync(0xffffffffu, mbar_wait(bar(x), parity, abort_flag, p.status, kStatusTimeoutProducer));
         };
-        // 8-byte stores: word (c, j) of a lane goes to row 16 b + g + 8 (j & 1) [keys], dims 16 ks + 4 t4 .. with ks = 2 (c ^ odd) +
+        // 8-byte stores: word (c, j) of a lane goes to row 16 b + g + 8 (j & 1) [keys], dims 16 ks + 4 t4 .. with ks = 2 c +
         // j / 2; or [values] to dim 16 (2 c + j / 2) + g + 8 (j & 1), stored tokens 16 b + 4 t4 ..
         uint32_t k_at[2][2];   // [c & 1][j / 2]
 #pragma unroll
         for (uint32_t c = 0; c < 2; ++c)
 #pragma unroll
             for (uint32_t j = 0; j < 2; ++j)
-                k_at[c][j] = base + kOffK + (16u * b + g) * 128u + (((2u * (2u * (c ^ odd) + j) + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u;
+                k_at[c][j] = base + kOffK + (16u * b + g) * 128u + (((2u * (2u * c + j) + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u;
         const uint32_t v_at = base + kOffV + (b >> 2) * kBlock + g * 128u + (((2u * (b & 3u) + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u;
         while (more) {
             const uint32_t cur_scales = scales, cur_left = left;
             if (cur_left > 0u) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(blk + kQ8ValueOff) + lane;
+                const uint4 *src = reinterpret_cast<const uint4 *>(blk + kQ8ValueOff) + place;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) cv[c] = __ldcg(src + 32 * c);
             }
