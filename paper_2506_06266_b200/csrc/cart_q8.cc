@@ -389,6 +389,12 @@ constexpr int kStreamPieceTiles = 1;
 // What a chain's piece costs a block beside its tiles (its rows fetched, its result written), in tile times.
 constexpr uint32_t kPieceTiles = 3;
 
+// Where a plan has work for both kernels they run at the same time, on blocks of their own.  What a block does its work in,
+// in ns per KV head: a tile of a chain, 16 tokens of a streamed row, one of its segments (128 rows that share 4096 tokens, 1 ..
+// 1024 of their own: 67 us one after the other, 49 side by side, with 24 / 32 / 48 / 64 / 80 blocks for the tiles
+// 74 / 60 / 49 / 56 / 60).  Neither kernel gets less than a quarter of the blocks: the rest can stream as fast as memory delivers.
+constexpr int64_t kTileNs = 1850, kTokenNs16 = 58, kSegNs = 400;
+
 // A part that this many rows of the stream or more name is worth a tcgen05 launch when together the rows would stream this
 // many tokens (times KV heads) of shared parts: the stream kernel does about 25 a nanosecond out of L2, and the launch, its
 // first tile and the merge that then is needed take some 20 us (128 rows over 4096 tokens: 70 us against 169 streamed; 8 rows
@@ -755,11 +761,22 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
     add_messages(&tp, st, cv, layer, messages, &w);
     sl->n_cta_used = 0;
     sl->n_unit_cta = 0;
+    int n_tile_cta = n_cta, n_stream_cta = n_cta;
+    if (!row_of.empty() && !tp.rows.empty() && n_cta > 1) {
+        // both kernels, side by side: blocks in proportion to their work
+        int64_t tiles = 0, tokens = 0;
+        for (const auto &t : tp.rows) tiles += t.n_tiles + kPieceTiles;
+        for (const cart_plan_seg &sg : segs) tokens += sg.n_tok;
+        const int64_t wt = kTileNs * tiles, ws = (kTokenNs16 * tokens >> 4) + kSegNs * (int64_t)segs.size();
+        n_tile_cta = (int)std::min<int64_t>(std::max<int64_t>(n_cta * wt / (wt + ws), n_cta / 4), n_cta - n_cta / 4);
+        n_tile_cta = std::min(std::max(n_tile_cta, 1), n_cta - 1);
+        n_stream_cta = n_cta - n_tile_cta;
+    }
     if (!row_of.empty()) {
         const size_t n_run = segs.size() * (size_t)Hkv;   // (as much as these rows can need)
-        items.resize(2 * n_run + (size_t)n_cta + 8);
-        merges.resize(row_of.size() * (size_t)Hkv + (size_t)n_cta);
-        cta.resize((size_t)n_cta + 1);
+        items.resize(2 * n_run + (size_t)n_stream_cta + 8);
+        merges.resize(row_of.size() * (size_t)Hkv + (size_t)n_stream_cta);
+        cta.resize((size_t)n_stream_cta + 1);
         cart_plan_out po{};
         po.items = items.data();
         po.items_cap = (int32_t)items.size();
@@ -768,7 +785,7 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
         po.merges_cap = (int32_t)merges.size();
         po.slots_cap = INT32_MAX;
         po.piece_cost = kStreamPieceTiles;
-        r = cart_plan_build_shared(segs.data(), sb.data(), (int32_t)row_of.size(), Hkv, cv.group, n_cta, kTileTokens, 0, kShareTileTokens, &po);
+        r = cart_plan_build_shared(segs.data(), sb.data(), (int32_t)row_of.size(), Hkv, cv.group, n_stream_cta, kTileTokens, 0, kShareTileTokens, &po);
         if (r != CART_OK) return ctx_fail(ctx, r, "q8 attention: planning failed (%s)", cart_status_string(r));
         items.resize((size_t)po.n_items);
         sl->n_cta_used = po.n_items > 0 ? po.n_cta_used : 0;
@@ -778,7 +795,7 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
     }
     // fewer blocks, and so fewer cuts, if the partial slots do not suffice
     bool placed = false;
-    for (uint64_t C = (uint64_t)n_cta;; C = (C + 1) / 2) {
+    for (uint64_t C = (uint64_t)n_tile_cta;; C = (C + 1) / 2) {
         if (!tp.rows.empty()) cut_chains(&tp, (uint32_t)Hkv, C);
         placed = place_partials(tp, (uint32_t)Hkv, n_rows, items, lay.slots_cap, &merges, &w, &st->count_tmp);
         if (placed || C == 1 || tp.rows.empty()) break;
@@ -854,6 +871,7 @@ cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t laye
         p.n_kv_heads = cv.cfg->n_kv_heads;
         p.n_q_heads = cv.cfg->n_q_heads;
         p.scale_log2 = scale_log2;
+        p.beside = sl->n_cta_used > 0;
         Q8_CUDA(ctx, q8_launch_tile(p, format, sl->n_unit_cta, s));
         ++*cv.launches;
     }
@@ -875,6 +893,7 @@ cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t laye
         p.group = cv.group;
         p.scale_log2 = scale_log2;
         p.grow = (uint32_t)grow;
+        p.beside = tiles;
         Q8_CUDA(ctx, q8_launch_stream(p, format, sl->n_cta_used, s));
         ++*cv.launches;
     }

@@ -443,7 +443,10 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
         acc += __shfl_sync(0xffffffffu, incl, 31);
     }
     uint32_t left_steps = hi - lo;
-    pdl_wait();  // the cache's last tokens, q, out and the partial slots belong to the kernels before until they are done
+    // The cache's last tokens, q, out and the partial slots belong to the kernels before until they are done.  Beside the tile
+    // kernel they are: all of its blocks have waited for them before this one could start.
+    if (p.beside) __threadfence();
+    else pdl_wait();
     const uint64_t once = l2_evict_first_policy();
 
     // ---- the issuing side: steps are requested in the order in which the warp will want them
@@ -771,7 +774,13 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
         }
     }
     __syncthreads();
-    if (*abort_flag != 0u) return;
+    const auto leave = [&]() {   // (what waits for this kernel waits for the tile kernel too)
+        if (p.beside) pdl_wait();
+    };
+    if (*abort_flag != 0u) {
+        leave();
+        return;
+    }
 
     // ---- pieces that belong together: one warp per (row group, head) ------------------------------------------
     uint32_t task = 0;
@@ -827,7 +836,10 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
     }
 
     // ---- row groups that other thread blocks hold parts of: at most the first and the last; whoever comes last merges
-    if (p.tickets == nullptr || item_begin == item_end) return;
+    if (p.tickets == nullptr || item_begin == item_end) {
+        leave();
+        return;
+    }
     __threadfence();
     __syncthreads();
     if (threadIdx.x < 2) {

@@ -61,6 +61,7 @@ struct Q8StreamParams {
     int32_t layer, group;
     float scale_log2;
     uint32_t grow;                   // tokens every cache has gained since the plan was built
+    uint32_t beside;                 // the tile kernel, launched just before, runs at the same time
 };
 
 struct Q8TileParams {                // the tcgen05 kernel: units as in cart_plan.h, all CART_UNIT_PAGED
@@ -79,6 +80,7 @@ struct Q8TileParams {                // the tcgen05 kernel: units as in cart_pla
     uint32_t *status;
     int32_t layer, group, n_kv_heads, n_q_heads;
     float scale_log2;
+    uint32_t beside;                 // the stream kernel, launched next, runs at the same time
 };
 
 cudaError_t q8_prepare_kernels();

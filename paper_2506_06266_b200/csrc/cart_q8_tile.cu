@@ -263,6 +263,8 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
 
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
+    // Beside the stream kernel this one passes on that the kernels before are done: the stream kernel does not wait.
+    if (p.beside) pdl_wait();
     pdl_launch_dependents();
     const uint32_t unit_begin = p.unit_cta_begin[blockIdx.x];
     const uint32_t unit_end = p.unit_cta_begin[blockIdx.x + 1];
