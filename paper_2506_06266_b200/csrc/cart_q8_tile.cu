@@ -436,11 +436,14 @@ __global__ void __launch_bounds__(kThreads, 1) cart_q8_tile_kernel(const Q8TileP
                 k_at[c][j] = base + kOffK + (16u * b + g) * 128u + (((2u * (2u * c + j) + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u;
         const uint32_t v_at = base + kOffV + (b >> 2) * kBlock + g * 128u + (((2u * (b & 3u) + (t4 >> 1)) ^ g) << 4) + (t4 & 1u) * 8u;
         while (more) {
-            const uint32_t cur_scales = scales, cur_left = left;
+            // (the scales are waited for before the values are requested -- a shuffle, so that it stays in place: behind the
+            // request the wait covers both)
+            const uint32_t cur_scales = __shfl_sync(0xffffffffu, scales, 0), cur_left = left;
             if (cur_left > 0u) {
                 const uint4 *src = reinterpret_cast<const uint4 *>(blk + kQ8ValueOff) + place;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) cv[c] = __ldcg(src + 32 * c);
+                for (int c = 0; c < 4; ++c)
+                    asm volatile("ld.global.cg.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(cv[c].x), "=r"(cv[c].y), "=r"(cv[c].z), "=r"(cv[c].w) : "l"(src + 32 * c));
             }
             const uint32_t ek = cur_scales & 0xFFu, ev = cur_scales >> 8;
             const bool none = cur_left == 0u || ev == kQ8NoScale;   // no values here: zeros
