@@ -197,9 +197,8 @@ cart_status make_state(cart_ctx *ctx)
     return CART_OK;
 }
 
-Cache *get(cart_ctx *ctx, cart_q8 id)
+Cache *get(Q8State *st, cart_q8 id)
 {
-    Q8State *st = *ctx_view(ctx).q8;
     if (!st || id < 0 || (size_t)id >= st->caches.size() || !st->caches[(size_t)id].live) return nullptr;
     return &st->caches[(size_t)id];
 }
@@ -217,6 +216,7 @@ void drop_pages(cart_ctx *ctx, Q8State *st, Cache &c, size_t keep)
 // Takes pages until the cache has room for `tokens`.  False: the arena is full (what was taken stays with the cache).
 bool take_pages(cart_ctx *ctx, Q8State *st, Cache &c, int64_t tokens)
 {
+    if (c.cap() >= tokens) return true;
     const uint64_t rows = page_bytes(*ctx_view(ctx).cfg) / kRowBytes;
     while (c.cap() < tokens) {
         uint64_t start = 0;
@@ -351,7 +351,7 @@ cart_status prepare_write(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int3
     had->clear();
     *n_tokens = 0;
     for (int32_t i = 0; i < n_ids; ++i) {
-        Cache *c = get(ctx, ids[i]);
+        Cache *c = get(st, ids[i]);
         if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "%s: ids[%d] is not an open cache", what, i);
         if (c->stamp == stamp) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "%s: ids[%d] appears twice", what, i);
         c->stamp = stamp;
@@ -981,7 +981,7 @@ cart_status cart_q8_open(cart_ctx *ctx, int32_t format, const cart_q8 *parts, in
         const CtxView cv = ctx_view(ctx);
         std::vector<int32_t> flat;
         for (int32_t i = 0; i < n_parts; ++i) {
-            const Cache *c = get(ctx, parts[i]);
+            const Cache *c = get(*cv.q8, parts[i]);
             if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_open: part %d is not an open cache", i);
             if (c->format != format) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_open: part %d is of another format", i);
             flat.insert(flat.end(), c->parts.begin(), c->parts.end());
@@ -1017,7 +1017,8 @@ cart_status cart_q8_close(cart_ctx *ctx, cart_q8 id)
 {
     if (!ctx) return CART_ERR_INVALID_ARG;
     return guarded(ctx, [&]() -> cart_status {
-        Cache *c = get(ctx, id);
+        const CtxView cv = ctx_view(ctx);
+        Cache *c = get(*cv.q8, id);
         if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_close: not an open cache");
         if (c->refs > 0) return ctx_fail(ctx, CART_ERR_IN_USE, "q8_close: %d caches stand behind it", c->refs);
         Q8State *st = *ctx_view(ctx).q8;
@@ -1077,7 +1078,7 @@ cart_status cart_q8_read(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32
         int64_t total = 0;
         int32_t format = 0;
         for (int32_t i = 0; i < n_ids; ++i) {
-            const Cache *c = get(ctx, ids[i]);
+            const Cache *c = get(*cv.q8, ids[i]);
             if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_read: ids[%d] is not an open cache", i);
             if (i == 0) format = c->format;
             if (c->format != format) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_read: the caches are of different formats");
@@ -1112,7 +1113,7 @@ cart_status cart_q8_attention(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, 
         int64_t rows = 0;
         int32_t format = 0;
         for (int32_t i = 0; i < n_ids; ++i) {
-            const Cache *c = get(ctx, ids[i]);
+            const Cache *c = get(*cv.q8, ids[i]);
             if (!c) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_attention: ids[%d] is not an open cache", i);
             if (i == 0) format = c->format;
             if (c->format != format) return ctx_fail(ctx, CART_ERR_INVALID_ARG, "q8_attention: the caches are of different formats");
@@ -1222,7 +1223,7 @@ cart_status cart_q8_len(cart_ctx *ctx, cart_q8 id, int32_t layer, int32_t *own, 
     if (!ctx) return CART_ERR_INVALID_ARG;
     return guarded(ctx, [&]() -> cart_status {
         const CtxView cv = ctx_view(ctx);
-        const Cache *c = get(ctx, id);
+        const Cache *c = get(*cv.q8, id);
         if (!c || layer < 0 || layer >= cv.cfg->n_layers) return ctx_fail(ctx, CART_ERR_BAD_HANDLE, "q8_len: bad handle");
         if (own) *own = c->len[(size_t)layer];
         if (total) {

@@ -27,18 +27,20 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t a)
     return (uint32_t)(max(e, kQ8MinExp) + 127);
 }
 
-// four values, already scaled, -> four stored codes (first value in the low byte)
+// four values times a power of two -> four stored codes (first value in the low byte)
 template <int kFmt>
-__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d)
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, float by)
 {
     if (kFmt == CART_Q8_INT8) {
-        // (no value leaves -127 .. 127: the scale is chosen so; conversion rounds half to even)
-        const uint32_t x = (uint32_t)(__float2int_rn(a) + 128), y = (uint32_t)(__float2int_rn(b) + 128);
-        const uint32_t z = (uint32_t)(__float2int_rn(c) + 128), w = (uint32_t)(__float2int_rn(d) + 128);
-        return x | (y << 8) | (z << 16) | (w << 24);
+        // No product leaves -127 .. 127 (the scale is chosen so), and it is exact: added to 1.5 * 2^23 + 128 it is rounded once,
+        // half to even, and the sum's low byte is the code plus 128.
+        const float up = 12582912.f + 128.f;
+        const uint32_t x = __float_as_uint(fmaf(a, by, up)), y = __float_as_uint(fmaf(b, by, up));
+        const uint32_t z = __float_as_uint(fmaf(c, by, up)), w = __float_as_uint(fmaf(d, by, up));
+        return __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
     }
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a * by, b * by), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c * by, d * by), __NV_SATFINITE, __NV_E4M3);
     return lo | (hi << 16);
 }
 
@@ -74,6 +76,10 @@ __device__ __forceinline__ void decode4(uint32_t r, float (&f)[4])
 // ---- write and read ------------------------------------------------------------------------------------
 // One thread block per block of 16 tokens, one warp at a time per (KV head, keys or values).  Both kernels move a few KB
 // per warp in 16-byte accesses and do little arithmetic: HBM bounds them for long ranges, the launch for short ones.
+// 100000 tokens of 8 KV heads written (616 MB moved) and read back (616 MB): 207 us, 5.9 TB/s.  What that hangs on is the
+// loads in flight: with 2, 3, 4 thread blocks of the write kernel resident (105, 85, 64 registers) it is 221, 207, 216, with
+// 2, 3, 4 of the read kernel 220, 219, 207.  (Staging that met the banks of shared memory 4 and 8 deep, and conversions
+// float -> int of the slow pipe, took 5 us together.)
 
 constexpr int kCopyThreads = 256;
 
@@ -123,8 +129,17 @@ __device__ __forceinline__ void words_to_rows(const uint32_t (&w)[4], bool upper
     b[1] = upper ? keep_b : got_b;
 }
 
+// Where lane l's 16 bytes of a chunk are staged: swapped about inside eights, so that the 4-byte (values) and 8-byte (keys)
+// accesses in row order fall on all banks.
+template <bool kValues>
+__device__ __forceinline__ uint32_t staged(uint32_t chunk, uint32_t l)
+{
+    const uint32_t x = kValues ? 2u * chunk + (l >> 4) : (chunk & 1u) + 4u * (chunk >> 1);
+    return chunk * 512u + (l ^ x) * 16u;
+}
+
 template <int kFmt>
-__global__ void __launch_bounds__(kCopyThreads) cart_q8_write_kernel(const __grid_constant__ Q8CopyParams p)
+__global__ void __launch_bounds__(kCopyThreads, 3) cart_q8_write_kernel(const __grid_constant__ Q8CopyParams p)
 {
     __shared__ __align__(16) uint8_t stage[kCopyThreads / 32][kQ8ValueOff];
     pdl_launch_dependents();
@@ -177,15 +192,15 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_write_kernel(const __gri
             float f[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                f[2 * j] = __uint_as_float(w[j] << 16) * down;
-                f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u) * down;
+                f[2 * j] = __uint_as_float(w[j] << 16);
+                f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
             }
             if (eb == kQ8NoScale) {  // (0 * NaN is not 0)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = 0.f;
             }
-            code[i][0] = encode4<kFmt>(f[0], f[1], f[2], f[3]);
-            code[i][1] = encode4<kFmt>(f[4], f[5], f[6], f[7]);
+            code[i][0] = encode4<kFmt>(f[0], f[1], f[2], f[3], down);
+            code[i][1] = encode4<kFmt>(f[4], f[5], f[6], f[7], down);
         }
         // to the stored order, through shared memory
         __syncwarp();
@@ -197,21 +212,23 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_write_kernel(const __gri
                 const uint32_t chunk = c16 >> 2, word = 2u * ((c16 >> 1) & 1u) + (c16 & 1u), dg = upper ? 4u : 0u;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    *reinterpret_cast<uint32_t *>(st + chunk * 512u + ((dg + j) * 4u + i) * 16u + word * 4u) = w[j];
+                    *reinterpret_cast<uint32_t *>(st + staged<true>(chunk, (dg + j) * 4u + i) + word * 4u) = w[j];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {   // rows 2 i (+ 1) and 8 further: neighbouring words
                 const uint32_t row = 2u * i + (upper ? 1u : 0u);
-                const uint32_t chunk = c16 >> 2, word = 2u * ((c16 >> 1) & 1u) + (row >> 3), l0 = (row & 7u) * 4u + 2u * (c16 & 1u);
-                *reinterpret_cast<uint32_t *>(st + chunk * 512u + l0 * 16u + word * 4u) = code[i][0];
-                *reinterpret_cast<uint32_t *>(st + chunk * 512u + (l0 + 1u) * 16u + word * 4u) = code[i][1];
+                const uint32_t chunk = c16 >> 2, word = 2u * ((c16 >> 1) & 1u), l0 = row * 4u + 2u * (c16 & 1u);
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j)
+                    *reinterpret_cast<uint2 *>(st + staged<false>(chunk, l0 + j) + word * 4u) = make_uint2(code[i][j], code[i + 4][j]);
             }
         }
         __syncwarp();
         uint4 mine[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mine[c] = *reinterpret_cast<const uint4 *>(st + c * 512 + lane * 16);
+        for (uint32_t c = 0; c < 4; ++c)
+            mine[c] = *reinterpret_cast<const uint4 *>(st + (is_v ? staged<true>(c, (uint32_t)lane) : staged<false>(c, (uint32_t)lane)));
         if (kept > 0u) {
             // codes held already stay, rounded once more if the scale has grown
             const uint32_t g = (uint32_t)lane >> 2, t = (uint32_t)lane & 3u;
@@ -236,7 +253,7 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_write_kernel(const __gri
                     if (grown > 0 && eb != kQ8NoScale) {
                         float v[4];
                         decode4<kFmt>(o[j], v);
-                        o[j] = encode4<kFmt>(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+                        o[j] = encode4<kFmt>(v[0], v[1], v[2], v[3], f);
                     }
                     n[j] = (o[j] & mask[j & 1]) | (n[j] & ~mask[j & 1]);
                 }
@@ -251,16 +268,18 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_write_kernel(const __gri
 }
 
 template <int kFmt>
-__global__ void __launch_bounds__(kCopyThreads) cart_q8_read_kernel(const __grid_constant__ Q8CopyParams p)
+__global__ void __launch_bounds__(kCopyThreads, 4) cart_q8_read_kernel(const __grid_constant__ Q8CopyParams p)
 {
     __shared__ __align__(16) uint8_t stage[kCopyThreads / 32][kQ8ValueOff];
-    pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Q8Entry e = find_entry(p, blockIdx.x);
     const uint32_t b = e.first / kQ8Block + (blockIdx.x - e.task_begin);
     const uint32_t page = __ldg(p.pages + e.list + b / (kTileTokens / kQ8Block));
     const uint32_t tok0 = b * kQ8Block, end = e.first + e.n;
     pdl_wait();
+    // (Only now: with the next kernels of a loop of steps resident before this one has run -- all that stands between are
+    // waits -- a step over shared parts took 94 us instead of 74.)
+    pdl_launch_dependents();
     uint8_t *st = stage[warp];
     const bool upper = lane >= 16;
     const uint32_t c16 = (uint32_t)lane & 15u;
@@ -277,7 +296,8 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_read_kernel(const __grid
         const float up = eb == kQ8NoScale ? __uint_as_float(0x7FC00000u) : exp2_int((int)eb - 127);
         __syncwarp();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(st + c * 512 + lane * 16) = x[c];
+        for (uint32_t c = 0; c < 4; ++c)
+            *reinterpret_cast<uint4 *>(st + (is_v ? staged<true>(c, (uint32_t)lane) : staged<false>(c, (uint32_t)lane))) = x[c];
         __syncwarp();
         uint32_t code[8][2];
         const uint32_t chunk = c16 >> 2;
@@ -288,16 +308,20 @@ __global__ void __launch_bounds__(kCopyThreads) cart_q8_read_kernel(const __grid
                 uint32_t w[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    w[j] = *reinterpret_cast<const uint32_t *>(st + chunk * 512u + ((dg + j) * 4u + i) * 16u + word * 4u);
+                    w[j] = *reinterpret_cast<const uint32_t *>(st + staged<true>(chunk, (dg + j) * 4u + i) + word * 4u);
                 words_to_rows(w, upper, code[i], code[i + 4]);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {
                 const uint32_t row = 2u * i + (upper ? 1u : 0u);
-                const uint32_t word = 2u * ((c16 >> 1) & 1u) + (row >> 3), l0 = (row & 7u) * 4u + 2u * (c16 & 1u);
-                code[i][0] = *reinterpret_cast<const uint32_t *>(st + chunk * 512u + l0 * 16u + word * 4u);
-                code[i][1] = *reinterpret_cast<const uint32_t *>(st + chunk * 512u + (l0 + 1u) * 16u + word * 4u);
+                const uint32_t word = 2u * ((c16 >> 1) & 1u), l0 = row * 4u + 2u * (c16 & 1u);
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j) {
+                    const uint2 y = *reinterpret_cast<const uint2 *>(st + staged<false>(chunk, l0 + j) + word * 4u);
+                    code[i][j] = y.x;
+                    code[i + 4][j] = y.y;
+                }
             }
         }
         __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(const_cast<void *>(is_v ? p.v : p.k)) + (int64_t)h * p.head_stride + 8 * c16;
