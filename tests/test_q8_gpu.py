@@ -523,6 +523,57 @@ def test_a_step_is_a_write_and_an_attention_over_many_steps_and_pages(pair):
             p.check_stored(c, 1)
 
 
+@pytest.mark.parametrize("fmt,hq,hkv,users,n", [("int8", 8, 4, 100, (1601,)), ("e4m3", 16, 8, 48, (900, 800))])
+def test_steps_over_shared_parts_enqueued_back_to_back(pair, fmt, hq, hkv, users, n):
+    # The tile kernel and the stream kernel run side by side, and the next call's kernels become resident before they are done:
+    # nothing is waited for on the host, and what stands in `out` right behind each step is kept.
+    steps = 70
+    p = pair(hq, hkv, fmt, rows=users, mb=160)
+    z = [p.open() for _ in n]
+    p.write(z, [rand((m, hkv, 128), m, 4) for m in n], [rand((m, hkv, 128), m + 9, 4) for m in n])
+    ids = [p.open(z) for _ in range(users)]
+    own = [(29 * i) % 200 + 1 for i in range(users)]
+    p.write(ids, [rand((m, hkv, 128), 60 + m) for m in own], [rand((m, hkv, 128), 70 + m) for m in own])
+    k, v = rand((steps, users, hkv, 128), 1, 3).to(DEV), rand((steps, users, hkv, 128), 2, 3).to(DEV)
+    q = rand((steps, users, hq, 128), 3).to(DEV)
+    out, lse = torch.empty((users, hq, 128), dtype=torch.bfloat16, device=DEV), torch.empty((users, hq), device=DEV)
+    k_back, v_back = torch.empty_like(k), torch.empty_like(v)
+    outs, lses = [], []
+    torch.cuda.synchronize()
+    before = B.cart_launch_count(p.ctx)
+    for t in range(steps):
+        B.cart_q8_decode_step(p.ctx, 0, ids, k[t], v[t], q[t], out, lse)
+        if t % 2:
+            outs.append(out.clone())
+            lses.append(lse.clone())
+        B.cart_q8_read(p.ctx, 0, ids, [m + t for m in own], [1] * users, k_back[t], v_back[t])
+        if not t % 2:
+            outs.append(out.clone())
+            lses.append(lse.clone())
+    B.cart_sync_status(p.ctx)
+    assert B.cart_launch_count(p.ctx) - before == 5 * steps   # write, tiles, stream, merge, read
+    some = list(range(0, users, 9))
+    for t in range(steps):
+        for i in some:
+            p.ref[ids[i]][0].write(f64(k[t, i:i + 1]), f64(v[t, i:i + 1]))
+            assert same(f64(k_back[t, i:i + 1]), p.ref[ids[i]][0].values(0)[-1:])
+        if t % 10 in (0, 9):
+            p.check([ids[i] for i in some], q[t, some], outs[t][some], lses[t][some])
+
+
+def test_the_same_cache_many_times_over_shared_parts(pair):
+    p = pair(8, 8, "int8", rows=80, mb=96)
+    z = p.open()
+    p.write([z], [rand((2000, 8, 128), 1, 4)], [rand((2000, 8, 128), 2, 4)])
+    a, b = p.open([z]), p.open([z])
+    p.write([a, b], [rand((90, 8, 128), 3), rand((1, 8, 128), 4)], [rand((90, 8, 128), 5), rand((1, 8, 128), 6)])
+    ids = [a] * 37 + [b, a, b]
+    q = rand((40, 8, 128), 7)
+    p.attend_and_check(ids, q, extra=1)
+    q[1:37] = q[0]
+    p.attend_and_check(ids, q)
+
+
 def test_results_repeat_bit_for_bit(pair):
     p = pair(16, 2, mb=96)
     ids = [p.open() for _ in range(3)]
