@@ -25,8 +25,9 @@
  *
  * Conventions are those of cart.h: host-side checks before anything is launched, statuses, errors by cart_last_error,
  * streams, one driving thread and stream at a time, device memory from the arena only.  Tensors are bf16, head_dim =
- * 128.  The calls run on the context's device whichever device is current.  They keep lengths on the host and upload page lists as these change, so they cannot be
- * captured into a CUDA graph: on a stream that is being captured they return CART_ERR_INVALID_ARG.
+ * 128.  The calls run on the context's device whichever device is current.  They keep lengths on the host and upload page
+ * lists as these change, so they cannot be captured into a CUDA graph: on a stream that is being captured they return
+ * CART_ERR_INVALID_ARG.
  */
 #ifndef CART_Q8_H_
 #define CART_Q8_H_
@@ -97,9 +98,11 @@ CART_API cart_status cart_q8_read(cart_ctx *ctx, int32_t layer, const cart_q8 *i
  * out; n_new[i] may exceed its own length only by being 1 (a query over the parts alone).  q and out are device bf16
  * [sum of n_new][n_q_heads][128], lse device fp32 [sum of n_new][n_q_heads] (natural log) or NULL: rows back to back,
  * cache after cache; nothing behind the last row is touched.  ids, n_new are host arrays; duplicate handles are allowed.
- * Parts that many rows of the batch have in common are read once for up to 128 / G of them (as cart_set_share_min_readers
- * says for cart_decode_attention).  Sums, maxima and the output are kept in fp32; results are bitwise reproducible for
- * the same sequence of calls.  A query row that holds a NaN or an infinity gives NaN.
+ * Parts that at least cart_set_share_min_readers rows of the batch have in common are read once for up to 2 * (128 / G) of
+ * them and multiplied on the tensor cores, as messages of four rows or more are, where that saves more than the second
+ * kernel costs; rows then stream the rest beside it (cart_set_side_by_side).  Sums, maxima and the output are kept in
+ * fp32; results are bitwise reproducible for the same sequence of calls.  A query row that holds a NaN or an infinity
+ * gives NaN.  out and lse may not overlap q.
  * Errors: INVALID_ARG, BAD_HANDLE, EMPTY (a row would see no token), CAPACITY (more rows than max_requests, or more
  * pages than a call can list), CUDA. */
 CART_API cart_status cart_q8_attention(cart_ctx *ctx, int32_t layer, const cart_q8 *ids /*host*/, int32_t n_ids,

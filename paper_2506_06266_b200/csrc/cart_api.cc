@@ -2067,13 +2067,10 @@ CtxView ctx_view(cart_ctx *ctx)
     v.scale = ctx->scale;
     v.n_cta = ctx->n_cta;
     v.share_min_readers = ctx->share_min_readers;
-    v.piece_cost = ctx->piece_cost;
-    v.unit_cost = kUnitCostTiles;
     v.side_by_side = ctx->side_by_side;
     v.max_grow = ctx->max_grow;
     v.launches = &ctx->launches;
     v.status = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(ctx->cfg.arena) + ctx->lay.status_off);
-    v.n_rows = ctx->n_rows;
     v.q8 = &ctx->q8;
     return v;
 }

@@ -213,10 +213,9 @@ struct CtxView {
     int group;               // G
     float scale;             // softmax scale
     int n_cta;               // SMs
-    int share_min_readers, piece_cost, unit_cost, side_by_side, max_grow;
+    int share_min_readers, side_by_side, max_grow;
     uint64_t *launches;
     uint32_t *status;        // device status word
-    uint64_t n_rows;         // rows of 256 bytes in the arena
     Q8State **q8;            // owned by the context, released by q8_release
 };
 CtxView ctx_view(cart_ctx *ctx);

@@ -87,6 +87,7 @@ struct Slot {
     int32_t n_items = 0, n_merges = 0, n_cta_used = 0;
     uint64_t unit_cta_off = 0, units_off = 0, readers_off = 0, slots_off = 0;   // the tcgen05 kernel's
     int32_t n_unit_cta = 0;
+    bool beside = false;   // both kernels at the same time
 };
 
 // Work for the tcgen05 kernel, as its tables want it.
@@ -389,11 +390,23 @@ constexpr int kStreamPieceTiles = 1;
 // What a chain's piece costs a block beside its tiles (its rows fetched, its result written), in tile times.
 constexpr uint32_t kPieceTiles = 3;
 
-// Where a plan has work for both kernels they run at the same time, on blocks of their own.  What a block does its work in,
-// in ns per KV head: a tile of a chain, 16 tokens of a streamed row, one of its segments (128 rows that share 4096 tokens, 1 ..
-// 1024 of their own: 67 us one after the other, 49 side by side, with 24 / 32 / 48 / 64 / 80 blocks for the tiles
-// 74 / 60 / 49 / 56 / 60).  Neither kernel gets less than a quarter of the blocks: the rest can stream as fast as memory delivers.
-constexpr int64_t kTileNs = 1850, kTokenNs16 = 58, kSegNs = 400;
+// Where a plan has work for both kernels they run at the same time, on blocks of their own (cart_set_side_by_side).  What a
+// block does its work in, in ns per KV head: a tile of a chain, 16 tokens of a streamed row, one of its segments.
+constexpr int64_t kTileNs = 2000, kTokenNs16 = 58, kSegNs = 400;
+
+// The blocks that the tile kernel gets of n.  In proportion to the work; but what would get less than a quarter of them gets
+// up to twice as many, since the model leaves out what a kernel's end takes, and a stream needs no more than three quarters
+// of the blocks to be as fast as memory.  (128 rows that share 4096 tokens, 1 .. 1024 of their own: 67 us one after the other,
+// side by side with 24 / 32 / 48 / 64 / 80 blocks for the tiles 74 / 60 / 49 / 56 / 60.  96 steps behind 2 of 16 parts of 2048
+// tokens, with 64 / 96 / 112 / 128 blocks: 95 / 82 / 79 / 109, the proportion being 124.)
+int tile_blocks(int n, int64_t tile_work, int64_t stream_work)
+{
+    int x = (int)((int64_t)n * tile_work / std::max<int64_t>(tile_work + stream_work, 1));
+    if (x < n / 4) x = std::min(n / 4, 2 * x + 1);
+    int rest = n - x;
+    if (rest < n / 4) rest = std::min(n / 4, 2 * rest + 1);
+    return std::min(std::max(n - rest, 1), n - 1);
+}
 
 // A part that this many rows of the stream or more name is worth a tcgen05 launch when together the rows would stream this
 // many tokens (times KV heads) of shared parts: the stream kernel does about 25 a nanosecond out of L2, and the launch, its
@@ -641,6 +654,7 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
         lens.push_back(c.len[(size_t)layer]);
     }
     key.push_back(cv.share_min_readers);
+    key.push_back(cv.side_by_side);
     for (Slot &sl : st->slots) {
         if (sl.kind != (decode ? kDecode : kMessage) || sl.epoch != st->epoch || sl.key != key) continue;
         if (decode ? cart_plan_reusable(sl.lens.data(), lens.data(), n_ids, cv.max_grow, grow) != 0 : sl.lens == lens) {
@@ -762,14 +776,13 @@ cart_status plan_slot(cart_ctx *ctx, int32_t layer, const cart_q8 *ids, int32_t 
     sl->n_cta_used = 0;
     sl->n_unit_cta = 0;
     int n_tile_cta = n_cta, n_stream_cta = n_cta;
-    if (!row_of.empty() && !tp.rows.empty() && n_cta > 1) {
-        // both kernels, side by side: blocks in proportion to their work
+    sl->beside = !row_of.empty() && !tp.rows.empty() && n_cta > 1 && cv.side_by_side > 0;
+    if (sl->beside) {
         int64_t tiles = 0, tokens = 0;
         for (const auto &t : tp.rows) tiles += t.n_tiles + kPieceTiles;
         for (const cart_plan_seg &sg : segs) tokens += sg.n_tok;
-        const int64_t wt = kTileNs * tiles, ws = (kTokenNs16 * tokens >> 4) + kSegNs * (int64_t)segs.size();
-        n_tile_cta = (int)std::min<int64_t>(std::max<int64_t>(n_cta * wt / (wt + ws), n_cta / 4), n_cta - n_cta / 4);
-        n_tile_cta = std::min(std::max(n_tile_cta, 1), n_cta - 1);
+        n_tile_cta = cv.side_by_side > 1 ? std::min(cv.side_by_side, n_cta - 1)
+                                         : tile_blocks(n_cta, kTileNs * tiles, (kTokenNs16 * tokens >> 4) + kSegNs * (int64_t)segs.size());
         n_stream_cta = n_cta - n_tile_cta;
     }
     if (!row_of.empty()) {
@@ -871,7 +884,7 @@ cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t laye
         p.n_kv_heads = cv.cfg->n_kv_heads;
         p.n_q_heads = cv.cfg->n_q_heads;
         p.scale_log2 = scale_log2;
-        p.beside = sl->n_cta_used > 0;
+        p.beside = sl->beside;
         Q8_CUDA(ctx, q8_launch_tile(p, format, sl->n_unit_cta, s));
         ++*cv.launches;
     }
@@ -893,7 +906,7 @@ cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t laye
         p.group = cv.group;
         p.scale_log2 = scale_log2;
         p.grow = (uint32_t)grow;
-        p.beside = tiles;
+        p.beside = sl->beside;
         Q8_CUDA(ctx, q8_launch_stream(p, format, sl->n_cta_used, s));
         ++*cv.launches;
     }

@@ -561,6 +561,32 @@ def test_steps_over_shared_parts_enqueued_back_to_back(pair, fmt, hq, hkv, users
             p.check([ids[i] for i in some], q[t, some], outs[t][some], lses[t][some])
 
 
+def test_every_division_of_the_blocks(pair):
+    # both kernels one after the other, side by side as planned, with the fewest and the most blocks for either; little work for
+    # the one beside much for the other
+    p = pair(8, 4, "e4m3", rows=700, mb=96)
+    z = p.open()
+    p.write([z], [rand((1600, 4, 128), 1, 4)], [rand((1600, 4, 128), 2, 4)])
+    ids = [p.open([z]) for _ in range(100)]
+    own = [(17 * i) % 70 + 1 for i in range(100)]
+    p.write(ids, [rand((m, 4, 128), 60 + m) for m in own], [rand((m, 4, 128), 70 + m) for m in own])
+    long = [p.open() for _ in range(2)]
+    p.write(long, [rand((6000, 4, 128), 3), rand((10, 4, 128), 4)], [rand((6000, 4, 128), 5), rand((10, 4, 128), 6)])
+    batches = ((ids, [1] * 100), ([long[0], long[1]], [600, 1]), ([long[0], long[1]], [1, 5]))
+    most = torch.cuda.get_device_properties(0).multi_processor_count - 1
+    for who, new in batches:
+        q = rand((sum(new), 8, 128), 9)
+        for mode in (0, 1, 2, 60, most):
+            B.cart_set_side_by_side(p.ctx, mode)
+            out, lse = p.attend(who, q, new, extra=1)
+            if mode == 0:
+                first = out
+                p.check(who, q, out, lse, new)
+            else:
+                assert float((first.float() - out.float()).norm() / out.float().norm()) < 0.01
+    B.cart_set_side_by_side(p.ctx, 1)
+
+
 def test_the_same_cache_many_times_over_shared_parts(pair):
     p = pair(8, 8, "int8", rows=80, mb=96)
     z = p.open()
