@@ -408,11 +408,10 @@ int tile_blocks(int n, int64_t tile_work, int64_t stream_work)
     return std::min(std::max(n - rest, 1), n - 1);
 }
 
-// A part that this many rows of the stream or more name is worth a tcgen05 launch when together the rows would stream this
-// many tokens (times KV heads) of shared parts: the stream kernel does about 25 a nanosecond out of L2, and the launch, its
-// first tile and the merge that then is needed take some 20 us (128 rows over 4096 tokens: 70 us against 169 streamed; 8 rows
-// over 2048: 30 against 15).
-constexpr int64_t kShareTokens = 600000;
+// Shared parts are worth a tcgen05 launch when together the rows would stream this many tokens (times KV heads) of them: the
+// launch, its first tile and the merge that then is needed cost some 15 us.  (8 KV heads, streamed and shared: 8 rows over
+// 4096 tokens 20 and 21 us, 32 over 1024 22 and 19, 16 over 4096 28 and 24, 64 over 1024 35 and 27, 8 over 16384 41 and 34.)
+constexpr int64_t kShareTokens = 300000;
 constexpr int32_t kShareMinLen = 64;   // a shorter part is half of a tile at most
 
 // The tcgen05 kernel's work (cart_plan.h): rows of messages that stand behind the same parts, and rows that share a part, are
