@@ -363,6 +363,10 @@ __global__ void __launch_bounds__(kCopyThreads, 4) cart_q8_read_kernel(const __g
 // was), and one barrier at the kernel's end later the pieces that belong together are combined.  (Dealing the blocks of
 // every row group out to all warps and combining after each cost about 4 us per row group and block: 64 requests of
 // 2048 + 1 .. 512 tokens took 61 us, 128 suffixes of 1 .. 1024 tokens 55.)
+//
+// HBM bounds it: 8 requests of 100000 tokens (8 KV heads, 1.64 GB) 249 us, 6.6 TB/s; 64 of 2048 + 1 .. 512 (300 MB) 57, 5.3
+// TB/s; one of 131071 (269 MB) 53.  Some 11 us of a launch are its start (work list, page list, first data hang on one
+// another) and its end (pieces, tickets, the last merge).
 constexpr int kWarps = 8;
 constexpr int kStages = 3;
 constexpr int kStreamThreads = kWarps * 32;
