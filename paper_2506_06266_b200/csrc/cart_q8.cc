@@ -917,7 +917,7 @@ cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t laye
         mp.out = out;
         mp.lse = lse;
         mp.group = cv.group;
-        Q8_CUDA(ctx, launch_merge(mp, sl->n_merges, s));
+        Q8_CUDA(ctx, q8_launch_join(mp, sl->n_merges, s));
         ++*cv.launches;
     }
     return CART_OK;

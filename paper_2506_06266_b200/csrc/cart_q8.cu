@@ -898,7 +898,71 @@ __global__ void __launch_bounds__(kStreamThreads, 1) cart_q8_stream_kernel(const
     }
 }
 
+// ---- joining partials ------------------------------------------------------------------------------------
+// out = sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M) over a row's partials.  A warp takes a query row, a lane four of its dims;
+// the numbers of four partials are requested together with their log-sum-exps, and most rows have no more: one trip to L2
+// behind the kernels before.  (The bf16 kernels' merge, which looks for the maximum first, added 11.0 us to six ragged
+// messages and 6.8 to one of 512 rows, this adds 8.6 and 5.3.)
+constexpr int kJoinWarps = 8;
+constexpr uint32_t kJoinSlots = 4;
+
+__global__ void __launch_bounds__(kJoinWarps * 32) cart_q8_join_kernel(const MergeParams p, uint32_t n)
+{
+    pdl_launch_dependents();
+    const uint32_t w = blockIdx.x * (uint32_t)kJoinWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31u, G = (uint32_t)p.group;
+    if (w >= n) return;
+    const uint32_t h = w % G;
+    const cart_merge_item mi = p.merges[w / G];   // (uploaded before the kernels whose partials are joined here were launched)
+    pdl_wait();
+    float M = -INFINITY, L = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t s0 = mi.slot_begin; s0 < mi.slot_end; s0 += kJoinSlots) {
+        float l[kJoinSlots];
+        float4 v[kJoinSlots];
+#pragma unroll
+        for (uint32_t j = 0; j < kJoinSlots; ++j) {
+            const bool in = s0 + j < mi.slot_end;
+            l[j] = in ? __ldcg(p.part_lse2 + (size_t)(s0 + j) * kMaxGroup + h) : -INFINITY;
+            v[j] = in ? __ldcg(reinterpret_cast<const float4 *>(p.part_o + ((size_t)(s0 + j) * G + h) * kHeadDim) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        // (a partial without keys has lse = -inf and weighs nothing; a NaN takes no part in the maximum and stays in the sums)
+        const float was = M;
+#pragma unroll
+        for (uint32_t j = 0; j < kJoinSlots; ++j) M = fmaxf(M, l[j]);
+        const float ref = M == -INFINITY ? 0.f : M, f = fast_exp2(was - ref);
+        L *= f;
+        a.x *= f;
+        a.y *= f;
+        a.z *= f;
+        a.w *= f;
+#pragma unroll
+        for (uint32_t j = 0; j < kJoinSlots; ++j) {
+            const float x = fast_exp2(l[j] - ref);
+            L += x;
+            a.x += x * v[j].x;
+            a.y += x * v[j].y;
+            a.z += x * v[j].z;
+            a.w += x * v[j].w;
+        }
+    }
+    const float inv = 1.f / L;
+    const size_t row = (size_t)mi.row_group * G + h;
+    uint2 packed;
+    packed.x = pack_bf16(a.x * inv, a.y * inv);
+    packed.y = pack_bf16(a.z * inv, a.w * inv);
+    *(reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + row * kHeadDim) + lane) = packed;
+    if (lane == 0u && p.lse) p.lse[row] = (M + log2f(L)) * 0.6931471805599453f;
+}
+
 }  // namespace
+
+cudaError_t q8_launch_join(const MergeParams &p, int n_merges, cudaStream_t s)
+{
+    cudaLaunchAttribute attr;
+    const uint32_t n = (uint32_t)n_merges * (uint32_t)p.group;
+    const cudaLaunchConfig_t cfg = pdl_config((int)((n + kJoinWarps - 1) / kJoinWarps), kJoinWarps * 32, 0, s, &attr);
+    return cudaLaunchKernelEx(&cfg, cart_q8_join_kernel, p, n);
+}
 
 cudaError_t q8_prepare_kernels()
 {

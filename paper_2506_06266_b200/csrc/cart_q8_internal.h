@@ -88,6 +88,7 @@ cudaError_t q8_prepare_tile_kernels();
 cudaError_t q8_launch_tile(const Q8TileParams &p, int format, int grid, cudaStream_t s);
 cudaError_t q8_launch_write(const Q8CopyParams &p, uint32_t n_tasks, cudaStream_t s);
 cudaError_t q8_launch_read(const Q8CopyParams &p, uint32_t n_tasks, cudaStream_t s);
+cudaError_t q8_launch_join(const MergeParams &p, int n_merges, cudaStream_t s);
 cudaError_t q8_launch_stream(const Q8StreamParams &p, int format, int grid, cudaStream_t s);
 
 }  // namespace cart
