@@ -899,7 +899,7 @@ cart_status launch_attention(cart_ctx *ctx, Slot *sl, int32_t grow, int32_t laye
         p.part_o = part_o;
         p.part_lse2 = part_lse2;
         p.merges = merges;
-        p.tickets = merge_after ? nullptr : reinterpret_cast<uint32_t *>(st->base);
+        p.tickets = merge_after || sl->n_merges == 0 ? nullptr : reinterpret_cast<uint32_t *>(st->base);  // (beside: never)
         p.status = cv.status;
         p.layer = layer;
         p.group = cv.group;

@@ -61,7 +61,7 @@ struct Q8StreamParams {
     int32_t layer, group;
     float scale_log2;
     uint32_t grow;                   // tokens every cache has gained since the plan was built
-    uint32_t beside;                 // the tile kernel, launched just before, runs at the same time
+    uint32_t beside;                 // the tile kernel, launched just before, runs at the same time (tickets: null)
 };
 
 struct Q8TileParams {                // the tcgen05 kernel: units as in cart_plan.h, all CART_UNIT_PAGED

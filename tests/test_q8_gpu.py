@@ -561,6 +561,30 @@ def test_steps_over_shared_parts_enqueued_back_to_back(pair, fmt, hq, hkv, users
             p.check([ids[i] for i in some], q[t, some], outs[t][some], lses[t][some])
 
 
+def test_a_message_and_a_user_that_decodes_with_nothing_to_join(pair):
+    # the stream kernel is done long before the tile kernel, and no merge follows: what is enqueued behind the call must find both done
+    p = pair(8, 1, "int8", rows=200)
+    ids = [p.open(), p.open()]
+    n = (250, 20)
+    p.write(ids, [rand((m, 1, 128), m) for m in n], [rand((m, 1, 128), m + 1) for m in n])
+    new = [30, 1]
+    q = rand((31, 8, 128), 3)
+    dev = q.to(DEV)
+    out, lse = torch.empty_like(dev), torch.empty((31, 8), device=DEV)
+    kept = []
+    before = B.cart_launch_count(p.ctx)
+    for _ in range(50):
+        out.fill_(5.0)
+        lse.fill_(5.0)
+        B.cart_q8_attention(p.ctx, 0, ids, dev, out, lse, n_new=new)
+        kept.append((out.clone(), lse.clone()))
+    B.cart_sync_status(p.ctx)
+    assert B.cart_launch_count(p.ctx) - before == 100   # tiles, stream
+    for o, l in kept:
+        assert torch.equal(o, kept[0][0]) and torch.equal(l, kept[0][1])
+    p.check(ids, q, *kept[0], new)
+
+
 def test_every_division_of_the_blocks(pair):
     # both kernels one after the other, side by side as planned, with the fewest and the most blocks for either; little work for
     # the one beside much for the other
