@@ -449,14 +449,33 @@ def cart_decode_attention_static(q, kv, n_reqs: int, n_q_heads: int, n_kv_heads:
 
 # ---- caches in 8 bits (include/cart_q8.h) ----------------------------------------------------------------------------
 
-def _q8_tensor(x, name: str) -> None:
-    """A torch tensor handed to the 8-bit calls must be what the C side takes it for: bf16, dense (addresses are trusted)."""
+_bf16 = None   # torch.bfloat16, once a tensor has shown it (its name takes longer to ask for than a call's other checks)
+
+
+def _is_bf16(x) -> bool:
+    global _bf16
+    if _bf16 is None and str(x.dtype) == "torch.bfloat16":
+        _bf16 = x.dtype
+    return x.dtype is _bf16
+
+
+def _q8_ptr(x, name: str) -> Optional[int]:
+    """The address of a torch tensor handed to the 8-bit calls, which must be what the C side takes it for: bf16, dense
+    (addresses are trusted)."""
     if not hasattr(x, "data_ptr"):
-        return
-    if str(x.dtype) != "torch.bfloat16":
+        return _ptr(x)
+    if not _is_bf16(x):
         raise ValueError("%s must be bfloat16, not %s" % (name, x.dtype))
     if not x.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
+    return x.data_ptr()
+
+
+def _q8_lse(x) -> Optional[int]:
+    """The address of a torch tensor for log-sum-exps: fp32, dense."""
+    if x is not None and hasattr(x, "data_ptr") and (x.element_size() != 4 or not x.is_floating_point() or not x.is_contiguous()):
+        raise ValueError("lse must be float32 and contiguous, not %s" % x.dtype)
+    return _ptr(x)
 
 
 def _counts(xs, n: int, name: str):
@@ -508,11 +527,12 @@ def cart_q8_write(ctx: int, layer: int, ids, n_tokens, k, v, first=None, strides
         if k is None:
             strides = (0, 0)
         else:
-            if str(k.dtype) != "torch.bfloat16" or k.dtype != v.dtype:
+            if not (_is_bf16(k) and _is_bf16(v)):
                 raise ValueError("k and v must be bfloat16, not %s and %s" % (k.dtype, v.dtype))
-            if k.dim() != 3 or k.stride() != v.stride() or k.shape != v.shape or k.shape[2] != 128 or k.stride(2) != 1:
+            step, shape = k.stride(), k.shape
+            if len(step) != 3 or step != v.stride() or shape != v.shape or shape[2] != 128 or step[2] != 1:
                 raise ValueError("k and v must be [tokens][KV heads][128] of equal strides, dense in the last dimension")
-            strides = (k.stride(0), k.stride(1))
+            strides = step[:2]
     _check(load_library().cart_q8_write(ctx, int(layer), arr, n, _counts(first, n, "first"), _counts(n_tokens, n, "n_tokens"),
                                         _ptr(k), _ptr(v), int(strides[0]), int(strides[1]), _stream(stream)),
            "cart_q8_write", ctx)
@@ -520,26 +540,21 @@ def cart_q8_write(ctx: int, layer: int, ids, n_tokens, k, v, first=None, strides
 
 def cart_q8_read(ctx: int, layer: int, ids, first, n_tokens, k, v, stream=None) -> None:
     arr, n = _reqs(ids)
-    _q8_tensor(k, "k")
-    _q8_tensor(v, "v")
     _check(load_library().cart_q8_read(ctx, int(layer), arr, n, _counts(first, n, "first"), _counts(n_tokens, n, "n_tokens"),
-                                       _ptr(k), _ptr(v), _stream(stream)), "cart_q8_read", ctx)
+                                       _q8_ptr(k, "k"), _q8_ptr(v, "v"), _stream(stream)), "cart_q8_read", ctx)
 
 
 def cart_q8_attention(ctx: int, layer: int, ids, q, out, lse=None, n_new=None, stream=None) -> None:
     arr, n = _reqs(ids)
-    _q8_tensor(q, "q")
-    _q8_tensor(out, "out")
-    _check(load_library().cart_q8_attention(ctx, int(layer), arr, n, _counts(n_new, n, "n_new"), _ptr(q), _ptr(out), _ptr(lse),
-                                            _stream(stream)), "cart_q8_attention", ctx)
+    _check(load_library().cart_q8_attention(ctx, int(layer), arr, n, _counts(n_new, n, "n_new"), _q8_ptr(q, "q"),
+                                            _q8_ptr(out, "out"), _q8_lse(lse), _stream(stream)), "cart_q8_attention", ctx)
 
 
 def cart_q8_decode_step(ctx: int, layer: int, ids, k_new, v_new, q, out, lse=None, first=None, stream=None) -> None:
     arr, n = _reqs(ids)
-    for x, name in ((k_new, "k_new"), (v_new, "v_new"), (q, "q"), (out, "out")):
-        _q8_tensor(x, name)
-    _check(load_library().cart_q8_decode_step(ctx, int(layer), arr, n, _counts(first, n, "first"), _ptr(k_new), _ptr(v_new),
-                                              _ptr(q), _ptr(out), _ptr(lse), _stream(stream)), "cart_q8_decode_step", ctx)
+    _check(load_library().cart_q8_decode_step(ctx, int(layer), arr, n, _counts(first, n, "first"), _q8_ptr(k_new, "k_new"),
+                                              _q8_ptr(v_new, "v_new"), _q8_ptr(q, "q"), _q8_ptr(out, "out"), _q8_lse(lse),
+                                              _stream(stream)), "cart_q8_decode_step", ctx)
 
 
 def cart_q8_len(ctx: int, cid: int, layer: int) -> Tuple[int, int]:

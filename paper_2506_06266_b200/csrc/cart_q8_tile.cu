@@ -37,7 +37,7 @@
 // written once): unrolled they overflowed the instruction cache that the roles share -- a third of its requests missed --
 // and a tile of a pair of M-tiles took 5.7 us.
 // What it takes: a tile of a pair of M-tiles 2.3 to 2.6 us (4400 to 4900 cycles), a chain's begin and end about 5 us, the first
-// scores 6; six ragged messages (1274 rows of 32 heads) 164 us with the merge = 580 TFLOP/s.  Nothing is busy for more than
+// scores 6; six ragged messages (1274 rows of 32 heads) 161 us with the joining = 590 TFLOP/s.  Nothing is busy for more than
 // 0.4 of that (tensor pipe 0.38, exponentials 0.39; issue slots 0.54): a half's scores, softmax and P V follow one another, and
 // the hand-over from one to the next costs 450 cycles beside two M-tiles' worth of other work.
 //
