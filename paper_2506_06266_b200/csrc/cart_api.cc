@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "cart.h"
+#include "cart_ctx.h"
 #include "cart_internal.h"
 
 namespace {

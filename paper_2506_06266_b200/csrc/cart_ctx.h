@@ -1,0 +1,30 @@
+// What cart_api.cc lets the other host files see of a context.
+#ifndef CART_CTX_H_
+#define CART_CTX_H_
+
+#include "cart_internal.h"
+
+namespace cart {
+
+struct Q8State;  // cart_q8.cc
+struct CtxView {
+    const cart_config *cfg;
+    int group;               // G
+    float scale;             // softmax scale
+    int n_cta;               // SMs
+    int share_min_readers, side_by_side, max_grow;
+    uint64_t *launches;
+    uint32_t *status;        // device status word
+    Q8State **q8;            // owned by the context, released by q8_release
+};
+CtxView ctx_view(cart_ctx *ctx);
+cart_status ctx_fail(cart_ctx *ctx, cart_status st, const char *fmt, ...);
+bool ctx_arena_alloc(cart_ctx *ctx, uint64_t rows, uint64_t *start);
+void ctx_arena_free(cart_ctx *ctx, uint64_t start, uint64_t rows);
+// Where a registered Cartridge lies: BAD_HANDLE (a composition too), EVICTED, or OK.
+cart_status ctx_cartridge(cart_ctx *ctx, cart_id id, uint64_t *k_row, uint64_t *v_row, int32_t *p);
+void q8_release(Q8State *st);
+void q8_clear_tickets(cart_ctx *ctx);  // after a timeout: a block that gave up may have left arrival tickets behind
+
+}  // namespace cart
+#endif

@@ -2,6 +2,7 @@
 #ifndef CART_Q8_INTERNAL_H_
 #define CART_Q8_INTERNAL_H_
 
+#include "cart_ctx.h"
 #include "cart_internal.h"
 #include "cart_q8.h"
 
